@@ -11,6 +11,10 @@
  *   jenga_unpermute         z_thw = G^-1(z_blk)                   Eq. 2
  *   jenga_stage_switch      resolution switch between stages      Eq. 4
  *
+ * and what a transformer block has in front of that attention and behind it: layer norm and its gradient
+ * (jenga_layer_norm), matrix products in 8-bit floating point (jenga_quantize, jenga_matmul), rotary positions
+ * over time, height and width (jenga_rotary).
+ *
  * Conventions
  *   - All tensor arguments are DEVICE pointers unless a comment says "host".  The caller owns
  *     every tensor and every workspace; the library owns only what is inside a jenga_plan.
@@ -265,6 +269,163 @@ int jenga_forward(const jenga_plan* plan, const void* q_thw, const void* k_thw, 
 int jenga_stage_switch(const float* x_t, const float* eps_t, const float* eps_tilde, float* x_out,
                        int32_t channels, int32_t T_in, int32_t H_in, int32_t W_in, int32_t T_out,
                        int32_t H_out, int32_t W_out, float sigma_t, void* stream);
+
+/* ---- around the attention -------------------------------------------------------------------
+ *
+ * These calls need no plan and keep nothing; they only enqueue work on `stream`, on the device that is
+ * current, whose memory all device pointers have to be.  Configs are host pointers, read before the call
+ * returns.  Strides are in elements; values of a row, a head or a group lie next to each other.  A pointer
+ * to elements is a multiple of their size unless a comment asks for more; rows off the 16-byte grid are
+ * taken.  An output may lie over nothing else that the call reads or writes, except where a comment says so:
+ * JENGA_EINVAL.  Calls with no rows return JENGA_OK and touch nothing.
+ */
+
+/* Types of elements.  JENGA_E4M3: OCP 8-bit floating point, 4 exponent and 3 mantissa bits, no infinities. */
+typedef enum { JENGA_BF16 = 0, JENGA_F16 = 1, JENGA_F32 = 2, JENGA_E4M3 = 3 } jenga_type;
+
+/*
+ * 8-bit tensors.  A matrix of r rows and c columns is held as
+ *   values  e4m3 [r][C], C = c rounded up to a multiple of 128; the columns that fill up are 0.  16-byte aligned
+ *   scales  uint8 [r][S] (a block is 1 row x 128 columns) or [ceil(r / 128)][S] (128 x 128), S = ceil(c / 512) * 4;
+ *           byte e + 127 for the scale 2^e of a block; the bytes that fill up a row are 0.  4-byte aligned
+ * and stands for values * 2^e.  e is the least whole number >= -127 with |x| <= 448 * 2^e for all finite x of the
+ * block (0 where they are all 0): nothing saturates, and the only rounding is the one to e4m3, to nearest even.
+ * What is not finite becomes NaN.
+ */
+
+/*
+ * x -> 8-bit tensor with blocks of block_rows (1 or 128) rows and 128 columns.
+ *   x: x_type (JENGA_BF16, JENGA_F16 or JENGA_F32) [rows][cols], x_stride >= cols elements from row to row
+ * A matrix product takes its left operand with blocks of 1 row and its right one (weights) with 128; the
+ * transpose of a matrix with blocks of 128 x 128 holds the same values.
+ * JENGA_EINVAL: null or misaligned pointers, cols < 1, rows < 0, another block_rows; JENGA_EUNSUPPORTED: more
+ * than 2^17 columns or 2^30 rows.
+ */
+int jenga_quantize(const void* x, int64_t x_stride, int32_t x_type, int64_t rows, int32_t cols, int32_t block_rows,
+                   void* q, uint8_t* scale, void* stream);
+
+/* out = a b^T + bias.  m >= 0, n >= 1, k a positive multiple of 128 (the columns of both operands as held). */
+typedef struct {
+  int64_t m, out_stride; /* rows of a and out; elements between rows of out, >= n               */
+  int32_t n, k;          /* rows of b; columns of a and b                                       */
+  int32_t out_type;      /* JENGA_BF16, JENGA_F16 or JENGA_F32                                  */
+  int32_t reserved;      /* 0                                                                   */
+} jenga_matmul_config;
+
+/*
+ * Product of two 8-bit tensors:
+ *   out[i][j] = sum over blocks kb of 2^(ea[i][kb] + eb[j / 128][kb]) * sum over k in kb of a[i][k] b[j][k] + bias[j]
+ *   a, a_scale   : [m][k] with blocks of 1 x 128
+ *   b, b_scale   : [n][k] with blocks of 128 x 128
+ *   bias_or_null : float32 [n]
+ * Sums are float32 and rounded once.  For 16-bit results the f8 matrix core multiplies, which adds eight products
+ * at a time and cuts them off at 2^-13 of the largest of the eight (for normally distributed values 1.5e-5 of the
+ * result's norm); for float32 results the operands are widened, and nothing is cut off.
+ * The gradients are products of the same kind: of a, from out's gradient in rows of blocks and b's transpose; of b,
+ * from the transposes of out's gradient (blocks of 1 x 128) and of a (128 x 128).
+ * JENGA_EUNSUPPORTED: more than 2^23 tiles of 128 x 128, k above 2^17.
+ */
+int jenga_matmul(const jenga_matmul_config* cfg, const void* a, const uint8_t* a_scale, const void* b,
+                 const uint8_t* b_scale, const float* bias_or_null, void* out, void* stream);
+
+/*
+ * Layer norm over the columns of each row.  Rows come in groups of group_rows consecutive ones (the last may be
+ * short) that share a weight and a bias: all rows in one group are the ordinary affine norm, a group for each batch
+ * entry with weight_offset 1 the modulation of a diffusion transformer, (1 + scale) and shift.
+ */
+typedef struct {
+  int64_t rows, group_rows; /* >= 0; >= 1                                                       */
+  int64_t x_stride;         /* elements between rows of x (and dx), >= cols                     */
+  int64_t y_stride;         /* of y, or dy in the gradient, >= cols; JENGA_E4M3: cols rounded up to 128 */
+  int64_t param_stride;     /* between groups of weight and bias, >= cols                       */
+  int32_t cols;             /* 1 to 2^17                                                        */
+  int32_t x_type;           /* JENGA_BF16, JENGA_F16 or JENGA_F32                               */
+  int32_t y_type;           /* of y (or dy): x_type, or in the forward pass JENGA_E4M3          */
+  int32_t param_type;       /* of weight and bias: x_type or JENGA_F32                          */
+  float eps, weight_offset; /* finite, eps >= 0                                                 */
+} jenga_norm_config;
+
+/*
+ *   mu = mean(x)   r = 1 / sqrt(mean((x - mu)^2) + eps)   y = (x - mu) r (weight_offset + weight) + bias
+ *   weight, bias : param_type [groups][cols], or NULL for zeros
+ *   y            : [rows][cols]; may be x itself (same address, stride and type).  JENGA_E4M3: an 8-bit tensor with
+ *                  blocks of 1 x 128, its scales in y_scale (else NULL)
+ *   mean, rstd   : float32 [rows], mu and r for the gradient, or NULL
+ * Sums are float32, y is rounded once.
+ */
+int jenga_layer_norm(const jenga_norm_config* cfg, const void* x, const void* weight_or_null, const void* bias_or_null,
+                     void* y, uint8_t* y_scale_or_null, float* mean_or_null, float* rstd_or_null, void* stream);
+
+/*
+ * Its gradient, from dy and what the forward pass left in mean and rstd:
+ *   h = (x - mean) rstd   g = dy (weight_offset + weight)   dx = rstd (g - mean(g) - h mean(g h))
+ *   dweight[group] = sum over its rows of dy h   dbias[group] = sum of dy
+ *   dy              : x_type, y_stride elements between rows
+ *   dx              : x_type, x_stride elements between rows
+ *   dweight, dbias  : float32 [groups][cols] next to each other, fully overwritten, or NULL
+ *   workspace       : jenga_layer_norm_grad_workspace bytes, 256-byte aligned, contents undefined after; NULL if
+ *                     both of them are
+ * Sums are float32 and in an order that depends on the sizes alone: the same call gives the same bits.
+ * JENGA_EUNSUPPORTED: more than 2^20 groups.
+ */
+int jenga_layer_norm_grad(const jenga_norm_config* cfg, const void* x, const void* dy, const void* weight_or_null,
+                          const float* mean, const float* rstd, void* dx, float* dweight_or_null, float* dbias_or_null,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of its workspace (host only): (1024 + groups) * cols * 8. */
+int jenga_layer_norm_grad_workspace(const jenga_norm_config* cfg, uint64_t* bytes);
+
+/*
+ * Rotary positions over the axes of a T x H x W grid.  The first dim[0] channels of a head turn with the token's
+ * t, the next dim[1] with its h, the next dim[2] with its w, the rest stay as they are.  Pair i of an axis with d
+ * channels turns by (origin + step * cell) * theta^(-2i / d):  (x, y) -> (x cos - y sin, x sin + y cos).
+ */
+enum {
+  JENGA_ROTARY_HALVES = 1u, /* pair i of an axis is its channels i and i + d/2; else 2i and 2i + 1   */
+  JENGA_ROTARY_INVERSE = 2u /* turns back: the inverse, and the gradient                          */
+};
+typedef struct {
+  int32_t T, H, W;           /* cells, each >= 1, at most 2^24 together                          */
+  int32_t head_dim;          /* even, 2 to 1024                                                  */
+  int32_t dim[3];            /* channels of each axis: even, >= 0, together 2 to head_dim         */
+  int32_t type;              /* JENGA_BF16, JENGA_F16 or JENGA_F32                               */
+  double theta;              /* > 0                                                              */
+  double origin[3], step[3]; /* position of cell n of an axis: origin + step * n                 */
+  uint32_t flags;            /* JENGA_ROTARY_*                                                   */
+  uint32_t reserved;         /* 0                                                                */
+} jenga_rotary_config;
+
+/*
+ * cos and sin of every pair and cell, axis by axis: float32 [T][dim[0]/2][2], [H][dim[1]/2][2], [W][dim[2]/2][2] one
+ * behind the other, T dim[0] + H dim[1] + W dim[2] floats in HOST memory, from float64 angles.  The caller copies them
+ * to the device once per grid.  Host only.
+ */
+int jenga_rotary_table(const jenga_rotary_config* cfg, float* table);
+
+/* A tensor [batch][tokens][heads][head_dim] where its strides say; dst may be src itself (same address and strides). */
+typedef struct {
+  const void* src;
+  void* dst;
+  int64_t src_batch, src_token, src_head; /* elements, >= 0                                      */
+  int64_t dst_batch, dst_token, dst_head; /* no two elements of dst in one place                 */
+  int32_t heads, reserved;                /* >= 1; 0                                             */
+} jenga_rotary_tensor;
+
+/*
+ * Turns one or two tensors (Q and K) in one launch.  Angles and products are float32, results rounded once.
+ *   table   : of this grid, dims, theta, origin and step, on the device, 8-byte aligned
+ *   tensors : host array of `count` (1 or 2)
+ * The cell of a token:
+ *   plan and cells NULL : token n < T*H*W is cell n in (t,h,w) row-major order; tokens behind (text) are copied
+ *   plan                : curve side; position i has the cell of its token, text and pads are copied.  The plan has the
+ *                         same T, H and W, and tokens = N_pad
+ *   cells               : int32 [batch][tokens][3], the cell on each axis: sequences of several grids, padded batches.
+ *                         Channels of an axis where it is negative are copied; cells past the end are taken as the last
+ * JENGA_EUNSUPPORTED: more than 2^24 * 256 pairs a head and tensor.
+ */
+int jenga_rotary(const jenga_rotary_config* cfg, const jenga_plan* plan_or_null, const int32_t* cells_or_null,
+                 const float* table, const jenga_rotary_tensor* tensors, int32_t count, int64_t batch, int64_t tokens,
+                 void* stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* jenga_strerror(int status);

@@ -5,6 +5,7 @@
 #include <cmath>
 #include <cstring>
 #include <new>
+#include <utility>
 
 #include "jenga_internal.h"
 
@@ -67,9 +68,280 @@ StageTiles stage_switch_tiles(long long channels, int T_in, int H_in, int W_in, 
   return s;
 }
 
+// ---- arguments of the calls around the attention
+
+namespace {
+
+constexpr int64_t MOST_COLS = 1 << 17, MOST_ROWS = 1ll << 40, MOST_STRIDE = 1ll << 40;
+
+int type_size(int type) { return type == JENGA_F32 ? 4 : type == JENGA_E4M3 ? 1 : 2; }
+bool float_type(int type) { return type == JENGA_BF16 || type == JENGA_F16 || type == JENGA_F32; }
+bool aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
+
+// `rows` rows of `width` bytes, `pitch` bytes apart.
+struct Span {
+  const void* at;
+  int64_t rows, pitch, width;
+  __int128 end() const { return (__int128)(uintptr_t)at + (__int128)(rows - 1) * pitch + width; }
+};
+
+// Whether two spans share a byte.  Rows of the same pitch may lie between each other's (columns of one matrix).
+bool overlap(const Span& a, const Span& b) {
+  if (!a.at || !b.at || a.rows < 1 || b.rows < 1) return false;
+  if ((__int128)(uintptr_t)a.at >= b.end() || (__int128)(uintptr_t)b.at >= a.end()) return false;
+  if (a.pitch == b.pitch && a.pitch > 0 && a.rows > 1 && b.rows > 1) {
+    const int64_t p = a.pitch;
+    const int64_t d = (int64_t)((((__int128)(uintptr_t)b.at - (__int128)(uintptr_t)a.at) % p + p) % p);   // b's columns behind a's
+    if (d >= a.width && d + b.width <= p) return false;
+  }
+  return true;
+}
+
+int64_t groups_of(const jenga_norm_config& c) { return (c.rows + c.group_rows - 1) / c.group_rows; }
+
+int norm_config_ok(const jenga_norm_config& c) {
+  if (c.rows < 0 || c.group_rows < 1 || c.cols < 1) return JENGA_EINVAL;
+  if (!float_type(c.x_type) || !(float_type(c.y_type) || c.y_type == JENGA_E4M3) || !float_type(c.param_type)) return JENGA_EINVAL;
+  if (!std::isfinite(c.eps) || c.eps < 0.0f || !std::isfinite(c.weight_offset)) return JENGA_EINVAL;
+  if (c.x_stride < c.cols || c.y_stride < c.cols || c.param_stride < c.cols) return JENGA_EINVAL;
+  if (c.cols > MOST_COLS || c.rows > MOST_ROWS || c.group_rows > MOST_ROWS) return JENGA_EUNSUPPORTED;
+  if (c.x_stride > MOST_STRIDE || c.y_stride > MOST_STRIDE || c.param_stride > MOST_STRIDE) return JENGA_EUNSUPPORTED;
+  const __int128 lim = (__int128)1 << 60;   // bytes: offsets stay in 64 bits
+  if ((__int128)c.rows * c.x_stride > lim || (__int128)c.rows * c.y_stride > lim || (__int128)c.rows * c.param_stride > lim)
+    return JENGA_EUNSUPPORTED;
+  if (c.y_type != c.x_type && c.y_type != JENGA_E4M3) return JENGA_EUNSUPPORTED;
+  if (c.param_type != c.x_type && c.param_type != JENGA_F32) return JENGA_EUNSUPPORTED;
+  return JENGA_OK;
+}
+
+}  // namespace
+
+int norm_args_ok(const jenga_norm_config* c, const void* x, const void* weight, const void* bias, const void* y, const uint8_t* y_scale,
+                 const float* mean, const float* rstd) {
+  if (!c || !x || !y) return JENGA_EINVAL;
+  const int why = norm_config_ok(*c);
+  if (why != JENGA_OK) return why;
+  const bool e4m3 = c->y_type == JENGA_E4M3;
+  const int64_t padded = ((int64_t)c->cols + 127) / 128 * 128, scales = ((int64_t)c->cols + 511) / 512 * 4;
+  if (e4m3 != (y_scale != nullptr) || (e4m3 && (c->y_stride != padded || !aligned(y, 16) || !aligned(y_scale, 4)))) return JENGA_EINVAL;
+  const int xs = type_size(c->x_type), ys = type_size(c->y_type), ps = type_size(c->param_type);
+  if (!aligned(x, xs) || !aligned(y, ys) || !aligned(weight, ps) || !aligned(bias, ps) || !aligned(mean, 4) || !aligned(rstd, 4))
+    return JENGA_EINVAL;
+  if (c->rows == 0) return JENGA_OK;
+  const Span in[3] = {{x, c->rows, c->x_stride * xs, (int64_t)c->cols * xs},
+                      {weight, groups_of(*c), c->param_stride * ps, (int64_t)c->cols * ps},
+                      {bias, groups_of(*c), c->param_stride * ps, (int64_t)c->cols * ps}};
+  const Span out[4] = {{y, c->rows, c->y_stride * ys, e4m3 ? padded : (int64_t)c->cols * ys}, {y_scale, c->rows, scales, scales},
+                       {mean, 1, c->rows * 4, c->rows * 4}, {rstd, 1, c->rows * 4, c->rows * 4}};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 3; ++j)
+      if (overlap(out[i], in[j]) && !(i == 0 && j == 0 && x == y && !e4m3 && c->x_stride == c->y_stride)) return JENGA_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i], out[j])) return JENGA_EINVAL;
+  }
+  return JENGA_OK;
+}
+
+int norm_grad_args_ok(const jenga_norm_config* c, const void* x, const void* dy, const void* weight, const float* mean,
+                      const float* rstd, const void* dx, const float* dweight, const float* dbias, const void* workspace,
+                      size_t workspace_bytes) {
+  if (!c || !x || !dy || !mean || !rstd || !dx) return JENGA_EINVAL;
+  const int why = norm_config_ok(*c);
+  if (why != JENGA_OK) return why;
+  if (c->y_type != c->x_type) return JENGA_EUNSUPPORTED;
+  const int xs = type_size(c->x_type), ps = type_size(c->param_type);
+  if (!aligned(x, xs) || !aligned(dy, xs) || !aligned(dx, xs) || !aligned(weight, ps) || !aligned(mean, 4) || !aligned(rstd, 4) ||
+      !aligned(dweight, 4) || !aligned(dbias, 4))
+    return JENGA_EINVAL;
+  if (c->rows == 0) return JENGA_OK;
+  const int64_t groups = groups_of(*c);
+  if (groups > 1 << 20) return JENGA_EUNSUPPORTED;
+  uint64_t need = 0;
+  if (dweight || dbias) {
+    if (!workspace || !aligned(workspace, 256)) return JENGA_EINVAL;
+    need = (uint64_t)(1024 + groups) * c->cols * 8;
+    if (workspace_bytes < need) return JENGA_EWORKSPACE;
+  }
+  const int64_t width = (int64_t)c->cols * xs, sums = groups * c->cols * 4;
+  const Span in[5] = {{x, c->rows, c->x_stride * xs, width}, {dy, c->rows, c->y_stride * xs, width},
+                      {weight, groups, c->param_stride * ps, (int64_t)c->cols * ps}, {mean, 1, c->rows * 4, c->rows * 4},
+                      {rstd, 1, c->rows * 4, c->rows * 4}};
+  const Span out[4] = {{dx, c->rows, c->x_stride * xs, width}, {dweight, 1, sums, sums}, {dbias, 1, sums, sums},
+                       {need ? workspace : nullptr, 1, (int64_t)need, (int64_t)need}};
+  for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < 5; ++j)
+      if (overlap(out[i], in[j])) return JENGA_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i], out[j])) return JENGA_EINVAL;
+  }
+  return JENGA_OK;
+}
+
+int norm_grad_parts(const jenga_norm_config& c) {
+  const int64_t groups = groups_of(c), rows = std::min(c.rows, c.group_rows);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(512 / groups, (rows + 7) / 8));
+}
+
+int quantize_args_ok(const void* x, int64_t x_stride, int32_t x_type, int64_t rows, int32_t cols, int32_t block_rows, const void* q,
+                     const uint8_t* scale) {
+  if (!x || !q || !scale || rows < 0 || cols < 1 || x_stride < cols || (block_rows != 1 && block_rows != 128)) return JENGA_EINVAL;
+  if (!float_type(x_type) || !aligned(x, type_size(x_type)) || !aligned(q, 16) || !aligned(scale, 4)) return JENGA_EINVAL;
+  if (cols > MOST_COLS || rows > 1ll << 30 || x_stride > 1ll << 28) return JENGA_EUNSUPPORTED;
+  if (rows == 0) return JENGA_OK;
+  const int64_t size = type_size(x_type), padded = ((int64_t)cols + 127) / 128 * 128, scales = ((int64_t)cols + 511) / 512 * 4;
+  const Span from = {x, rows, x_stride * size, cols * size}, to = {q, rows, padded, padded},
+             bytes = {scale, block_rows == 1 ? rows : (rows + 127) / 128, scales, scales};
+  return overlap(from, to) || overlap(from, bytes) || overlap(to, bytes) ? JENGA_EINVAL : JENGA_OK;
+}
+
+int matmul_args_ok(const jenga_matmul_config* c, const void* a, const uint8_t* a_scale, const void* b, const uint8_t* b_scale,
+                   const float* bias, const void* out) {
+  if (!c || !a || !a_scale || !b || !b_scale || !out) return JENGA_EINVAL;
+  if (c->m < 0 || c->n < 1 || c->k < 1 || c->k % 128 != 0 || c->out_stride < c->n || c->reserved != 0) return JENGA_EINVAL;
+  if (!float_type(c->out_type)) return JENGA_EINVAL;
+  const int64_t size = type_size(c->out_type);
+  if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4) || !aligned(bias, 4) || !aligned(out, size))
+    return JENGA_EINVAL;
+  if (c->k > MOST_COLS || c->m > 1ll << 30 || c->out_stride > 1ll << 31) return JENGA_EUNSUPPORTED;
+  if ((c->m + 127) / 128 * (((int64_t)c->n + 127) / 128) > 1ll << 23) return JENGA_EUNSUPPORTED;
+  if (c->m == 0) return JENGA_OK;
+  const int64_t scales = ((int64_t)c->k + 511) / 512 * 4;
+  const Span to = {out, c->m, c->out_stride * size, c->n * size};
+  const Span in[5] = {{a, c->m, c->k, c->k}, {a_scale, c->m, scales, scales}, {b, c->n, c->k, c->k},
+                      {b_scale, ((int64_t)c->n + 127) / 128, scales, scales}, {bias, 1, (int64_t)c->n * 4, (int64_t)c->n * 4}};
+  for (const Span& s : in)
+    if (overlap(to, s)) return JENGA_EINVAL;
+  return JENGA_OK;
+}
+
+int rotary_config_ok(const jenga_rotary_config* c) {
+  if (!c) return JENGA_EINVAL;
+  if (c->T < 1 || c->H < 1 || c->W < 1 || c->head_dim < 1 || !float_type(c->type) || c->reserved != 0) return JENGA_EINVAL;
+  if (c->flags & ~(uint32_t)(JENGA_ROTARY_HALVES | JENGA_ROTARY_INVERSE)) return JENGA_EINVAL;
+  if (!std::isfinite(c->theta) || c->theta <= 0.0) return JENGA_EINVAL;
+  int64_t dims = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (!std::isfinite(c->origin[i]) || !std::isfinite(c->step[i])) return JENGA_EINVAL;
+    if (c->dim[i] < 0 || c->dim[i] % 2 != 0) return JENGA_EINVAL;
+    dims += c->dim[i];
+  }
+  if (dims < 1 || dims > c->head_dim) return JENGA_EINVAL;
+  const int64_t lim = 1ll << 24;
+  if (c->head_dim % 2 != 0 || c->head_dim > 1024) return JENGA_EUNSUPPORTED;
+  if (c->T > lim || c->H > lim || c->W > lim || (int64_t)c->T * c->H > lim || (int64_t)c->T * c->H * c->W > lim) return JENGA_EUNSUPPORTED;
+  return JENGA_OK;
+}
+
+namespace {
+
+// A tensor [batch][tokens][heads][head_dim] of one rotary call.
+struct Layout4 {
+  const void* at;
+  int64_t batch, token, head;   // strides
+  int64_t n[3];                 // batch, tokens, heads
+  int64_t width, size;          // head_dim, bytes of an element
+  int64_t end() const { return (n[0] - 1) * batch + (n[1] - 1) * token + (n[2] - 1) * head + width; }
+
+  // No two elements in one place: each stride, from the smallest on, steps over all that the smaller ones reach.
+  bool distinct() const {
+    int64_t stride[3] = {batch, token, head}, count[3] = {n[0], n[1], n[2]};
+    int64_t reach = width;
+    for (int left = 3; left > 0; --left) {
+      int best = 0;
+      for (int i = 1; i < left; ++i)
+        if (count[best] == 1 || (count[i] > 1 && stride[i] < stride[best])) best = i;
+      if (count[best] > 1) {
+        if (stride[best] < reach) return false;
+        reach += (count[best] - 1) * stride[best];
+      }
+      std::swap(stride[best], stride[left - 1]);
+      std::swap(count[best], count[left - 1]);
+    }
+    return true;
+  }
+  // The same bytes as rows of a common pitch, where the heads of a token lie within one token stride.
+  Span rows() const {
+    const int64_t row = (n[2] - 1) * head + width;
+    if (n[1] > 1 && row <= token && (n[0] == 1 || (batch % token == 0 && batch >= n[1] * token)))
+      return {at, n[0] == 1 ? n[1] : (n[0] - 1) * (batch / token) + n[1], token * size, row * size};
+    return {at, 1, end() * size, end() * size};
+  }
+};
+
+}  // namespace
+
+int rotary_args_ok(const jenga_rotary_config* c, const jenga_plan* plan, const int32_t* cells, const float* table,
+                   const jenga_rotary_tensor* tensors, int32_t count, int64_t batch, int64_t tokens) {
+  const int why = rotary_config_ok(c);
+  if (why != JENGA_OK) return why;
+  if (!table || !tensors || count < 1 || count > 2 || batch < 0 || tokens < 0 || (plan && cells)) return JENGA_EINVAL;
+  if (!aligned(table, 8) || !aligned(cells, 4)) return JENGA_EINVAL;
+  if (plan && (plan->cfg.T != c->T || plan->cfg.H != c->H || plan->cfg.W != c->W || plan->info.N_pad != tokens)) return JENGA_EINVAL;
+  if (batch > 1ll << 31 || tokens > 1ll << 31) return JENGA_EUNSUPPORTED;
+  if (batch > 0 && tokens > 0 && (__int128)batch * tokens * (c->head_dim / 2) > (__int128)0xFFFFFF00u) return JENGA_EUNSUPPORTED;
+  const int64_t size = type_size(c->type);
+  Layout4 src[2], dst[2];
+  for (int i = 0; i < count; ++i) {
+    const jenga_rotary_tensor& t = tensors[i];
+    if (!t.src || !t.dst || t.heads < 1 || t.reserved != 0 || !aligned(t.src, size) || !aligned(t.dst, size)) return JENGA_EINVAL;
+    const int64_t strides[6] = {t.src_batch, t.src_token, t.src_head, t.dst_batch, t.dst_token, t.dst_head};
+    for (const int64_t s : strides) {
+      if (s < 0) return JENGA_EINVAL;
+      if (s > MOST_STRIDE) return JENGA_EUNSUPPORTED;
+    }
+    if (t.heads > 65535 * 8) return JENGA_EUNSUPPORTED;
+    if (batch == 0 || tokens == 0) continue;
+    const __int128 lim = (__int128)1 << 60;
+    if ((__int128)t.src_batch * batch + (__int128)t.src_token * tokens + (__int128)t.src_head * t.heads > lim ||
+        (__int128)t.dst_batch * batch + (__int128)t.dst_token * tokens + (__int128)t.dst_head * t.heads > lim)
+      return JENGA_EUNSUPPORTED;
+    src[i] = {t.src, t.src_batch, t.src_token, t.src_head, {batch, tokens, t.heads}, c->head_dim, size};
+    dst[i] = {t.dst, t.dst_batch, t.dst_token, t.dst_head, {batch, tokens, t.heads}, c->head_dim, size};
+    if (!dst[i].distinct()) return JENGA_EINVAL;
+  }
+  if (batch == 0 || tokens == 0) return JENGA_OK;
+  const int64_t n_table = (int64_t)c->T * c->dim[0] + (int64_t)c->H * c->dim[1] + (int64_t)c->W * c->dim[2];
+  const Span angles = {table, 1, n_table * 4, n_table * 4}, where = {cells, 1, batch * tokens * 12, batch * tokens * 12};
+  for (int i = 0; i < count; ++i) {
+    const Span to = dst[i].rows();
+    if ((n_table > 0 && overlap(to, angles)) || overlap(to, where)) return JENGA_EINVAL;
+    for (int j = 0; j < count; ++j) {
+      const bool in_place = i == j && src[i].at == dst[i].at && (batch == 1 || src[i].batch == dst[i].batch) &&
+                            (tokens == 1 || src[i].token == dst[i].token) && (tensors[i].heads == 1 || src[i].head == dst[i].head);
+      if (!in_place && overlap(to, src[j].rows())) return JENGA_EINVAL;
+      if (j < i && overlap(to, dst[j].rows())) return JENGA_EINVAL;
+    }
+  }
+  return JENGA_OK;
+}
+
 }  // namespace jenga
 
 extern "C" {
+
+int jenga_layer_norm_grad_workspace(const jenga_norm_config* c, uint64_t* bytes) {
+  if (!c || !bytes) return JENGA_EINVAL;
+  const int why = jenga::norm_config_ok(*c);
+  if (why != JENGA_OK) return why;
+  if (jenga::groups_of(*c) > 1 << 20) return JENGA_EUNSUPPORTED;
+  *bytes = (uint64_t)(1024 + jenga::groups_of(*c)) * c->cols * 8;
+  return JENGA_OK;
+}
+
+int jenga_rotary_table(const jenga_rotary_config* c, float* table) {
+  const int why = jenga::rotary_config_ok(c);
+  if (why != JENGA_OK) return why;
+  if (!table) return JENGA_EINVAL;
+  const int cells[3] = {c->T, c->H, c->W};
+  for (int a = 0; a < 3; ++a)
+    for (int n = 0; n < cells[a]; ++n)
+      for (int i = 0; i < c->dim[a] / 2; ++i) {
+        const double angle = (c->origin[a] + c->step[a] * n) * std::pow(c->theta, -2.0 * i / c->dim[a]);
+        *table++ = (float)std::cos(angle);
+        *table++ = (float)std::sin(angle);
+      }
+  return JENGA_OK;
+}
 
 int jenga_plan_info(const jenga_plan* p, jenga_plan_info_t* info) {
   if (!p || !info) return JENGA_EINVAL;

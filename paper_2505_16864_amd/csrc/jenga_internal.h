@@ -164,6 +164,49 @@ struct StageTiles {
 // on_16: inputs 16-byte aligned
 StageTiles stage_switch_tiles(long long channels, int T_in, int H_in, int W_in, int T_out, int H_out, int W_out, bool on_16);
 
+// Tokens of a T x H x W grid (at most 2^24) to their cells, by multiplication: floor(n / d) = n * ceil(2^(24 + l) / d) >> (24 + l)
+// for n < 2^24 and 2^l >= d.
+struct GridCells {
+  int T, H, W;
+  uint32_t cells;
+  uint32_t by_w, by_h;
+  int shift_w, shift_h;
+  GridCells() = default;
+  GridCells(int t, int h, int w) : T(t), H(h), W(w), cells((uint32_t)t * (uint32_t)h * (uint32_t)w) {
+    factor(w, &by_w, &shift_w);
+    factor(h, &by_h, &shift_h);
+  }
+  static void factor(int d, uint32_t* by, int* shift) {
+    int l = 0;
+    while ((1ll << l) < d) ++l;
+    *shift = 24 + l;
+    *by = (uint32_t)(((1ull << *shift) + (uint64_t)d - 1) / (uint64_t)d);   // at most 2^25
+  }
+  JENGA_HOST_DEVICE void split(uint32_t n, int cell[3]) const {
+    const uint32_t th = (uint32_t)((uint64_t)n * by_w >> shift_w), t = (uint32_t)((uint64_t)th * by_h >> shift_h);
+    cell[0] = (int)t;
+    cell[1] = (int)(th - t * (uint32_t)H);
+    cell[2] = (int)(n - th * (uint32_t)W);
+  }
+};
+
+// Checks of arguments (jenga_host.cpp), all of a call's that need no device.  They return a jenga_status.
+int norm_args_ok(const jenga_norm_config* c, const void* x, const void* weight, const void* bias, const void* y, const uint8_t* y_scale,
+                 const float* mean, const float* rstd);
+int norm_grad_args_ok(const jenga_norm_config* c, const void* x, const void* dy, const void* weight, const float* mean,
+                      const float* rstd, const void* dx, const float* dweight, const float* dbias, const void* workspace,
+                      size_t workspace_bytes);
+int quantize_args_ok(const void* x, int64_t x_stride, int32_t x_type, int64_t rows, int32_t cols, int32_t block_rows, const void* q,
+                     const uint8_t* scale);
+int matmul_args_ok(const jenga_matmul_config* c, const void* a, const uint8_t* a_scale, const void* b, const uint8_t* b_scale,
+                   const float* bias, const void* out);
+int rotary_config_ok(const jenga_rotary_config* c);
+int rotary_args_ok(const jenga_rotary_config* c, const jenga_plan* plan, const int32_t* cells, const float* table,
+                   const jenga_rotary_tensor* tensors, int32_t count, int64_t batch, int64_t tokens);
+
+// Workgroups that share the rows of a group in the gradient of the norm.
+int norm_grad_parts(const jenga_norm_config& c);
+
 // Kernel launchers (defined in the .hip files).  All return a jenga_status.
 // 1 to 3 tensors of the plan's shape
 int launch_permute(const jenga_plan* p, const void* const* src, void* const* dst, int tensors, bool forward,
