@@ -13,7 +13,7 @@
  *
  * and what a transformer block has in front of that attention and behind it: layer norm and its gradient
  * (jenga_layer_norm), matrix products in 8-bit floating point (jenga_quantize, jenga_matmul), rotary positions
- * over time, height and width (jenga_rotary).
+ * over time, height and width (jenga_rotary, jenga_forward_rotary).
  *
  * Conventions
  *   - All tensor arguments are DEVICE pointers unless a comment says "host".  The caller owns
@@ -426,6 +426,21 @@ typedef struct {
 int jenga_rotary(const jenga_rotary_config* cfg, const jenga_plan* plan_or_null, const int32_t* cells_or_null,
                  const float* table, const jenga_rotary_tensor* tensors, int32_t count, int64_t batch, int64_t tokens,
                  void* stream);
+
+/*
+ * jenga_forward of Q and K turned by their rotary positions: jenga_rotary of both and jenga_forward, with the same results, in the
+ * launches of jenga_forward alone (the turn is part of the re-ordering pass).
+ *   rotary, table : as in jenga_rotary, of the plan's grid and head_dim and type JENGA_BF16
+ *   q, k, v_thw   : bf16 thw side, read only, consecutive tokens (of all batch entries) token_stride >= heads * head_dim
+ *                   elements apart: 3 * heads * head_dim for the columns of one projection, q, k and v_thw in the same rows
+ * Other arguments as in jenga_forward.  No output may lie over another tensor.
+ * JENGA_EUNSUPPORTED: more than 21845 batch entries, token_stride above 2^24.
+ */
+int jenga_forward_rotary(const jenga_plan* plan, const jenga_rotary_config* rotary, const float* table, const void* q_thw,
+                         const void* k_thw, const void* v_thw, int64_t token_stride, void* q_curve, void* k_curve,
+                         void* v_curve, int32_t* sel_count, int32_t* sel_index, uint8_t* mask_or_null,
+                         void* select_workspace, size_t select_workspace_bytes, void* out_curve, float* lse_or_null,
+                         void* attn_workspace, size_t attn_workspace_bytes, void* out_thw, void* stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* jenga_strerror(int status);

@@ -24,7 +24,7 @@ EXPORTS = ["jenga_plan_create", "jenga_plan_destroy", "jenga_plan_info", "jenga_
            "jenga_block_sparse_attn", "jenga_pack_kv",
            "jenga_block_sparse_attn_packed", "jenga_unpermute", "jenga_forward", "jenga_stage_switch",
            "jenga_quantize", "jenga_matmul", "jenga_layer_norm", "jenga_layer_norm_grad", "jenga_layer_norm_grad_workspace",
-           "jenga_rotary_table", "jenga_rotary", "jenga_strerror"]
+           "jenga_rotary_table", "jenga_rotary", "jenga_forward_rotary", "jenga_strerror"]
 
 
 class jenga_config(ctypes.Structure):
@@ -102,6 +102,8 @@ def _load():
     lib.jenga_rotary_table.argtypes = [ctypes.POINTER(jenga_rotary_config), vp]
     lib.jenga_rotary.argtypes = [ctypes.POINTER(jenga_rotary_config), vp, vp, vp, ctypes.POINTER(jenga_rotary_tensor), i32, i64,
                                  i64, vp]
+    lib.jenga_forward_rotary.argtypes = [vp, ctypes.POINTER(jenga_rotary_config)] + [vp] * 4 + [i64] + [vp] * 7 + [size, vp, vp, vp,
+                                                                                                                size, vp, vp]
     lib.jenga_strerror.argtypes = [ctypes.c_int]
     lib.jenga_strerror.restype = ctypes.c_char_p
     for name in EXPORTS[:-1]:
@@ -423,6 +425,25 @@ def jenga_rotary(cfg, table, q, q_out, k=None, k_out=None, cells=None, plan=None
     mine = jenga_rotary_config.from_buffer_copy(cfg)
     mine.type = _type(q, what)
     _check(_lib.jenga_rotary(ctypes.byref(mine), plan, _ptr(cells), _ptr(table), tensors, len(pairs), batch, tokens, stream), what)
+
+
+def jenga_forward_rotary(plan, cfg, table, q_thw, k_thw, v_thw, q_curve, k_curve, v_curve, sel_count, sel_index, mask,
+                         select_workspace, select_workspace_bytes, out_curve, lse, attn_workspace, attn_workspace_bytes, out_thw,
+                         stream=None):
+    """q_thw, k_thw, v_thw: [batch, N_v + N_c, heads, head_dim], tokens the same distance apart in all three."""
+    what = "jenga_forward_rotary"
+    batch, tokens, heads, dim = q_thw.shape
+    stride = q_thw.stride(1) if tokens > 1 else q_thw.stride(0) if batch > 1 else heads * dim
+    for t in (q_thw, k_thw, v_thw):
+        _need(t.shape == q_thw.shape and str(t.dtype) == "torch.bfloat16" and t.stride(3) == 1 and (heads == 1 or t.stride(2) == dim) and
+              (tokens == 1 or t.stride(1) == stride) and (batch == 1 or t.stride(0) == stride * tokens), what,
+              "shape %s, strides %s" % (tuple(t.shape), t.stride()))
+    _rotary_table(cfg, table, what)
+    _on_device(what, table, q_thw, k_thw, v_thw)
+    _check(_lib.jenga_forward_rotary(plan, ctypes.byref(cfg), _ptr(table), _ptr(q_thw), _ptr(k_thw), _ptr(v_thw), stride, _ptr(q_curve),
+                                     _ptr(k_curve), _ptr(v_curve), _ptr(sel_count), _ptr(sel_index), _ptr(mask),
+                                     _ptr(select_workspace), select_workspace_bytes, _ptr(out_curve), _ptr(lse),
+                                     _ptr(attn_workspace), attn_workspace_bytes, _ptr(out_thw), stream), what)
 
 
 def raw():

@@ -204,6 +204,51 @@ int jenga_forward(const jenga_plan* p, const void* q_thw, const void* k_thw, con
   return rc;
 }
 
+int jenga_forward_rotary(const jenga_plan* p, const jenga_rotary_config* rotary, const float* table, const void* q_thw,
+                         const void* k_thw, const void* v_thw, int64_t token_stride, void* q_curve, void* k_curve, void* v_curve,
+                         int32_t* sel_count, int32_t* sel_index, uint8_t* mask_or_null, void* select_workspace,
+                         size_t select_workspace_bytes, void* out_curve, float* lse_or_null, void* attn_workspace,
+                         size_t attn_workspace_bytes, void* out_thw, void* stream) {
+  if (!p || !table || !q_thw || !k_thw || !v_thw || !q_curve || !k_curve || !v_curve || !sel_count || !sel_index ||
+      !select_workspace || !out_curve || !attn_workspace || !out_thw)
+    return JENGA_EINVAL;
+  int rc = jenga::rotary_config_ok(rotary);
+  if (rc != JENGA_OK) return rc;
+  const jenga_config& c = p->cfg;
+  if (rotary->T != c.T || rotary->H != c.H || rotary->W != c.W || rotary->head_dim != c.head_dim || rotary->type != JENGA_BF16 ||
+      token_stride < (int64_t)c.heads * c.head_dim)
+    return JENGA_EINVAL;
+  if (!on_plan_device(p)) return JENGA_EINVAL;
+  if ((((uintptr_t)select_workspace | (uintptr_t)attn_workspace) & 255u) != 0 || ((uintptr_t)table & 7u) != 0) return JENGA_EINVAL;
+  if (select_workspace_bytes < p->info.select_workspace_bytes || attn_workspace_bytes < p->info.attn_workspace_bytes)
+    return JENGA_EWORKSPACE;
+  if (3ll * c.batch > 65535 || token_stride > 1 << 24) return JENGA_EUNSUPPORTED;
+  const size_t bh = (size_t)c.batch * c.heads, row = (size_t)c.head_dim * 2, M = (size_t)p->info.M;
+  const size_t tokens = (size_t)c.batch * (p->info.N_v + c.n_text), curve = bh * p->info.N_pad * row;
+  const size_t from = ((tokens - 1) * (size_t)token_stride + (size_t)c.heads * c.head_dim) * 2;
+  const size_t angles = ((size_t)c.T * rotary->dim[0] + (size_t)c.H * rotary->dim[1] + (size_t)c.W * rotary->dim[2]) * 4;
+  // what is written, then what is read; nothing written may lie over anything else
+  const struct { const void* at; size_t bytes; } all[14] = {
+      {q_curve, curve}, {k_curve, curve}, {v_curve, curve}, {out_curve, curve}, {out_thw, tokens * c.heads * row}, {sel_count, bh * M * 4},
+      {sel_index, bh * M * M * 4}, {mask_or_null, bh * M * M}, {lse_or_null, bh * p->info.N_pad * 4},
+      {select_workspace, p->info.select_workspace_bytes}, {attn_workspace, p->info.attn_workspace_bytes}, {q_thw, from}, {k_thw, from},
+      {v_thw, from}};
+  for (int i = 0; i < 11; ++i) {
+    if (!all[i].at) continue;
+    if (overlap(all[i].at, all[i].bytes, table, angles)) return JENGA_EINVAL;
+    for (int j = i + 1; j < 14; ++j)
+      if (all[j].at && overlap(all[i].at, all[i].bytes, all[j].at, all[j].bytes)) return JENGA_EINVAL;
+  }
+  const void* src[3] = {q_thw, k_thw, v_thw};
+  void* dst[3] = {q_curve, k_curve, v_curve};
+  rc = jenga::launch_permute_turn_pool(p, *rotary, table, src, token_stride, dst, select_workspace, stream);
+  if (rc == JENGA_OK)
+    rc = jenga::launch_select(p, q_curve, k_curve, sel_count, sel_index, mask_or_null, select_workspace, true, stream);
+  if (rc == JENGA_OK)
+    rc = attention(p, q_curve, k_curve, v_curve, sel_count, sel_index, out_curve, lse_or_null, attn_workspace, out_thw, stream);
+  return rc;
+}
+
 int jenga_pack_kv(const jenga_plan* p, const void* k, const void* v, void* workspace, size_t workspace_bytes,
                   void* stream) {
   if (!p || !k || !v || !workspace) return JENGA_EINVAL;

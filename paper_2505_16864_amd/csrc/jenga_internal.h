@@ -217,6 +217,9 @@ int launch_select(const jenga_plan* p, const void* q, const void* k, int32_t* se
                   int32_t* sel_index, uint8_t* mask, void* ws, bool pooled, void* stream);
 // Q, K and V into curve order, and the block means of Q and K into the selection's workspace.
 int launch_permute_pool(const jenga_plan* p, const void* const src[3], void* const dst[3], void* select_ws, void* stream);
+// The same with Q and K turned by their rotary positions on the way, from tensors whose tokens are token_stride elements apart.
+int launch_permute_turn_pool(const jenga_plan* p, const jenga_rotary_config& c, const float* table, const void* const src[3],
+                             int64_t token_stride, void* const dst[3], void* select_ws, void* stream);
 // Looks up the address of the static selection scratch on `device` (the current device) once.
 int select_scratch_init(int device);
 int launch_pack(const jenga_plan* p, const void* k, const void* v, void* ws, void* stream);

@@ -9,10 +9,19 @@
 
 #include "jenga_device.h"
 #include "jenga_internal.h"
+#include "jenga_pool.h"
 
 namespace {
 
 using namespace jenga;
+
+struct Turns {
+  const float2* table;
+  GridCells grid;
+  int pairs[3];   // of each axis
+  int base[3];    // of each axis in the table
+  float sign;     // -1: the inverse rotation
+};
 
 struct RotaryArgs {
   const void* src[2];
@@ -20,55 +29,158 @@ struct RotaryArgs {
   int64_t src_batch[2], src_token[2], src_head[2], dst_batch[2], dst_token[2], dst_head[2];
   int heads[2];
   int count;
-  const float2* table;
+  Turns turns;
   const int32_t *src_of_pos, *cells;
   int64_t tokens, units;   // units: batch * tokens
-  GridCells grid;
-  int pairs[3];            // of each axis
-  int base[3];             // of each axis in the table
   int head_dim;
   int heads_per_wg;
-  float sign;              // -1: the inverse rotation
 };
 
-// The cell of token n of batch entry b on each axis; false: not rotated.  -1 on an axis: its channels are not.
-__device__ __forceinline__ bool cells_of(const RotaryArgs& a, int64_t b, int64_t n, int cell[3]) {
+// A pair's place: its axis (3: none, it stays) and where cell 0 of it is in the table.
+struct Pair {
+  int axis, at, step;
+};
+
+// Channel c: the pair that it belongs to, the other channel of it, and whether it is the second one.
+template <bool HALVES>
+__device__ __forceinline__ Pair pair_of(const Turns& t, int c, int* other, bool* second) {
+  const int e0 = 2 * t.pairs[0], e1 = e0 + 2 * t.pairs[1], e2 = e1 + 2 * t.pairs[2];
+  Pair p;
+  p.axis = c < e0 ? 0 : c < e1 ? 1 : c < e2 ? 2 : 3;
+  const int start = p.axis == 0 ? 0 : p.axis == 1 ? e0 : e1, i = c - start;
+  p.step = p.axis == 0 ? t.pairs[0] : p.axis == 1 ? t.pairs[1] : t.pairs[2];
+  *second = HALVES ? i >= p.step : i & 1;
+  *other = p.axis == 3 ? c : HALVES ? (*second ? c - p.step : c + p.step) : c ^ 1;
+  p.at = (p.axis == 0 ? t.base[0] : p.axis == 1 ? t.base[1] : t.base[2]) + (HALVES ? (*second ? i - p.step : i) : i >> 1);
+  return p;
+}
+
+// cos and sin for a pair of a token in these cells; false: the pair stays as it is, to the last bit.
+__device__ __forceinline__ bool turn_of(const Turns& t, const Pair& p, const int cell[3], float2* turn) {
+  const int n = p.axis == 0 ? cell[0] : p.axis == 1 ? cell[1] : cell[2];
+  const bool turned = p.axis < 3 && n >= 0;
+  *turn = make_float2(1.f, 0.f);
+  if (turned) {
+    *turn = t.table[p.at + n * p.step];
+    turn->y *= t.sign;
+  }
+  return turned;
+}
+
+// The cell of token n of batch entry b on each axis, -1: not turned.
+__device__ __forceinline__ void cells_of(const RotaryArgs& a, int64_t b, int64_t n, int cell[3]) {
+  cell[0] = cell[1] = cell[2] = -1;
   if (a.cells) {
     const int32_t* c = a.cells + (b * a.tokens + n) * 3;
-    const int most[3] = {a.grid.T - 1, a.grid.H - 1, a.grid.W - 1};
-#pragma unroll
-    for (int i = 0; i < 3; ++i) cell[i] = min(c[i], most[i]);
-    return true;
+    cell[0] = min(c[0], a.turns.grid.T - 1);
+    cell[1] = min(c[1], a.turns.grid.H - 1);
+    cell[2] = min(c[2], a.turns.grid.W - 1);
+    return;
   }
   if (a.src_of_pos) n = a.src_of_pos[n];
-  if (n < 0 || n >= a.grid.cells) return false;
-  a.grid.split((uint32_t)n, cell);
-  return true;
+  if (n >= 0 && n < a.turns.grid.cells) a.turns.grid.split((uint32_t)n, cell);
 }
 
-// Channel c: its axis, pair and whether it is the pair's second one.  Axis 3: not rotated.
-struct Channel {
-  int axis, pair, second;
-};
-template <bool HALVES>
-__device__ __forceinline__ Channel channel(const RotaryArgs& a, int c) {
-  Channel r;
-  const int d0 = 2 * a.pairs[0], d1 = d0 + 2 * a.pairs[1], d2 = d1 + 2 * a.pairs[2];
-  r.axis = c < d0 ? 0 : c < d1 ? 1 : c < d2 ? 2 : 3;
-  const int i = c - (r.axis == 0 ? 0 : r.axis == 1 ? d0 : d1), half = r.axis == 0 ? a.pairs[0] : r.axis == 1 ? a.pairs[1] : a.pairs[2];
-  r.second = HALVES ? i >= half : i & 1;
-  r.pair = HALVES ? i - (r.second ? half : 0) : i >> 1;
-  return r;
+// Neighbours paired, head_dim a multiple of 8: a thread turns eight channels of a token, in registers, four heads at a time.
+template <typename X>
+__global__ __launch_bounds__(256) void rotary_neighbours_kernel(RotaryArgs a) {
+  const int pieces = a.head_dim / 8;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, unit = id / pieces;
+  if (unit >= a.units) return;
+  const int c = (int)(id - unit * pieces) * 8;
+  const int64_t b = unit / a.tokens, n = unit - b * a.tokens;
+  int cell[3];
+  cells_of(a, b, n, cell);
+  float2 turn[4];
+  bool turned[4], any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    int other;
+    bool second;
+    turned[i] = turn_of(a.turns, pair_of<false>(a.turns, c + 2 * i, &other, &second), cell, &turn[i]);
+    any |= turned[i];
+  }
+  const int h0 = blockIdx.y * a.heads_per_wg;
+  for (int k = 0; k < a.count; ++k) {
+    const X* src = (const X*)a.src[k] + b * a.src_batch[k] + n * a.src_token[k] + c;
+    X* dst = (X*)a.dst[k] + b * a.dst_batch[k] + n * a.dst_token[k] + c;
+    const int h1 = min(h0 + a.heads_per_wg, a.heads[k]);
+    if (!any && src == dst && a.src_head[k] == a.dst_head[k]) continue;   // in place: nothing to do
+    for (int h = h0; h < h1; h += 4) {
+      typename Eight<X>::raw raw[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (h + u < h1) raw[u] = *(const typename Eight<X>::raw*)(src + (h + u) * a.src_head[k]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (h + u >= h1) break;
+        f32x8 v = Eight<X>::wide(raw[u]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = v[2 * i], y = v[2 * i + 1];
+          v[2 * i] = turned[i] ? fmaf(x, turn[i].x, -(y * turn[i].y)) : x;
+          v[2 * i + 1] = turned[i] ? fmaf(x, turn[i].y, y * turn[i].x) : y;
+        }
+        *(typename Eight<X>::raw*)(dst + (h + u) * a.dst_head[k]) = Eight<X>::narrow(v);
+      }
+    }
+  }
 }
-__device__ __forceinline__ float2 turn_of(const RotaryArgs& a, const Channel& c, const int cell[3], bool rotated) {
-  if (!rotated || c.axis == 3) return make_float2(1.f, 0.f);
-  const int at = c.axis == 0 ? cell[0] : c.axis == 1 ? cell[1] : cell[2];
-  if (at < 0) return make_float2(1.f, 0.f);
-  const int pairs = c.axis == 0 ? a.pairs[0] : c.axis == 1 ? a.pairs[1] : a.pairs[2];
-  const int base = c.axis == 0 ? a.base[0] : c.axis == 1 ? a.base[1] : a.base[2];
-  float2 t = a.table[base + at * pairs + c.pair];
-  t.y *= a.sign;
-  return t;
+
+// Channels half an axis apart paired, head_dim a multiple of 8 up to 512: a thread turns eight channels of a token; the other channel
+// of each pair comes from the wavefront's LDS, where the lanes of a token put theirs.  (The two of a pair may lie anywhere against
+// the 16-byte pieces: an axis of 42 channels has halves of 21.)
+template <typename X>
+__global__ __launch_bounds__(256) void rotary_halves_kernel(RotaryArgs a) {
+  __shared__ __attribute__((aligned(16))) X room[4][4][64 * 8];   // wavefront, head
+  const int pieces = a.head_dim / 8, per_wave = 64 / pieces, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = lane / pieces, c = (lane - row * pieces) * 8;
+  const int64_t unit = ((int64_t)blockIdx.x * 4 + wave) * per_wave + row;
+  if (row >= per_wave || unit >= a.units) return;
+  const int64_t b = unit / a.tokens, n = unit - b * a.tokens;
+  int cell[3];
+  cells_of(a, b, n, cell);
+  float2 turn[8];
+  int other[8];
+  bool turned[8], any = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    bool second;
+    turned[i] = turn_of(a.turns, pair_of<true>(a.turns, c + i, &other[i], &second), cell, &turn[i]);
+    if (!second) turn[i].y = -turn[i].y;   // x cos - y sin, y cos + x sin
+    other[i] += row * a.head_dim;
+    any |= turned[i];
+  }
+  const int h0 = blockIdx.y * a.heads_per_wg;
+  for (int k = 0; k < a.count; ++k) {
+    const X* src = (const X*)a.src[k] + b * a.src_batch[k] + n * a.src_token[k] + c;
+    X* dst = (X*)a.dst[k] + b * a.dst_batch[k] + n * a.dst_token[k] + c;
+    const int h1 = min(h0 + a.heads_per_wg, a.heads[k]);
+    for (int h = h0; h < h1; h += 4) {
+      typename Eight<X>::raw raw[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (h + u < h1) raw[u] = *(const typename Eight<X>::raw*)(src + (h + u) * a.src_head[k]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (h + u < h1) __builtin_memcpy(&room[wave][u][row * a.head_dim + c], &raw[u], sizeof(raw[u]));
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (h + u >= h1) break;
+        f32x8 v = Eight<X>::wide(raw[u]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float y = (float)room[wave][u][other[i]];
+          v[i] = turned[i] ? fmaf(v[i], turn[i].x, y * turn[i].y) : v[i];
+        }
+        if (any || src != dst) *(typename Eight<X>::raw*)(dst + (h + u) * a.dst_head[k]) = Eight<X>::narrow(v);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
 }
 
 // Any even head_dim: a thread per pair of channels.
@@ -81,23 +193,27 @@ __global__ __launch_bounds__(256) void rotary_pairs_kernel(RotaryArgs a) {
   const int64_t b = unit / a.tokens, n = unit - b * a.tokens;
   int c0 = 2 * p, c1 = 2 * p + 1;
   if (HALVES) {   // pair p of the axis it falls on; behind the axes neighbours
-    const int e0 = a.pairs[0], e1 = e0 + a.pairs[1], e2 = e1 + a.pairs[2];
-    if (p < e0) c0 = p, c1 = p + a.pairs[0];
-    else if (p < e1) c0 = p + e0, c1 = c0 + a.pairs[1];
-    else if (p < e2) c0 = p + e1, c1 = c0 + a.pairs[2];
+    const int e0 = a.turns.pairs[0], e1 = e0 + a.turns.pairs[1], e2 = e1 + a.turns.pairs[2];
+    if (p < e0) c0 = p, c1 = p + a.turns.pairs[0];
+    else if (p < e1) c0 = p + e0, c1 = c0 + a.turns.pairs[1];
+    else if (p < e2) c0 = p + e1, c1 = c0 + a.turns.pairs[2];
   }
-  int cell[3] = {0, 0, 0};
-  const bool rotated = cells_of(a, b, n, cell);
-  const float2 t = turn_of(a, channel<HALVES>(a, c0), cell, rotated);
+  int cell[3], other;
+  bool second;
+  cells_of(a, b, n, cell);
+  float2 t;
+  const bool turned = turn_of(a.turns, pair_of<HALVES>(a.turns, c0, &other, &second), cell, &t);
   const int h0 = blockIdx.y * a.heads_per_wg;
   for (int k = 0; k < a.count; ++k) {
     const X* src = (const X*)a.src[k] + b * a.src_batch[k] + n * a.src_token[k];
     X* dst = (X*)a.dst[k] + b * a.dst_batch[k] + n * a.dst_token[k];
     const int h1 = min(h0 + a.heads_per_wg, a.heads[k]);
     for (int h = h0; h < h1; ++h) {
-      const float x = (float)src[h * a.src_head[k] + c0], y = (float)src[h * a.src_head[k] + c1];
-      dst[h * a.dst_head[k] + c0] = (X)(x * t.x - y * t.y);
-      dst[h * a.dst_head[k] + c1] = (X)(x * t.y + y * t.x);
+      const X *s = src + h * a.src_head[k];
+      X* d = dst + h * a.dst_head[k];
+      const X x = s[c0], y = s[c1];
+      d[c0] = turned ? (X)fmaf((float)x, t.x, -((float)y * t.y)) : x;
+      d[c1] = turned ? (X)fmaf((float)x, t.y, (float)y * t.x) : y;
     }
   }
 }
@@ -106,16 +222,160 @@ int status() { return hipGetLastError() == hipSuccess ? JENGA_OK : JENGA_EHIP; }
 
 template <typename X>
 int run_rotary(const RotaryArgs& a, bool halves, hipStream_t st) {
-  const int most = a.count > 1 ? std::max(a.heads[0], a.heads[1]) : a.heads[0];
-  const int64_t wgs = (a.units * (a.head_dim / 2) + 255) / 256;
-  if (wgs >= 1 << 24) return JENGA_EUNSUPPORTED;   // 2^32 threads are more than a grid has in x
-  const dim3 grid((unsigned)wgs, (most + a.heads_per_wg - 1) / a.heads_per_wg);
-  if (halves) rotary_pairs_kernel<X, true><<<grid, 256, 0, st>>>(a);
-  else rotary_pairs_kernel<X, false><<<grid, 256, 0, st>>>(a);
+  const int most = a.count > 1 ? std::max(a.heads[0], a.heads[1]) : a.heads[0], groups = (most + a.heads_per_wg - 1) / a.heads_per_wg;
+  const int pieces = a.head_dim / 8;
+  if (a.head_dim % 8 != 0 || (halves && pieces > 64)) {
+    const dim3 grid((unsigned)((a.units * (a.head_dim / 2) + 255) / 256), groups);
+    if (halves) rotary_pairs_kernel<X, true><<<grid, 256, 0, st>>>(a);
+    else rotary_pairs_kernel<X, false><<<grid, 256, 0, st>>>(a);
+  } else if (halves) {
+    const int64_t per_wg = 64 / pieces * 4;
+    rotary_halves_kernel<X><<<dim3((unsigned)((a.units + per_wg - 1) / per_wg), groups), 256, 0, st>>>(a);
+  } else {
+    rotary_neighbours_kernel<X><<<dim3((unsigned)((a.units * pieces + 255) / 256), groups), 256, 0, st>>>(a);
+  }
   return status();
 }
 
+Turns turns_of(const jenga_rotary_config& c, const float* table) {
+  Turns t;
+  t.table = (const float2*)table;
+  t.grid = GridCells(c.T, c.H, c.W);
+  const int cells[3] = {c.T, c.H, c.W};
+  for (int i = 0, base = 0; i < 3; ++i) {
+    t.pairs[i] = c.dim[i] / 2;
+    t.base[i] = base;
+    base += cells[i] * t.pairs[i];
+  }
+  t.sign = c.flags & JENGA_ROTARY_INVERSE ? -1.f : 1.f;
+  return t;
+}
+
+// ---- Q, K and V into curve order, Q and K turned on the way, with the block means of Q and K: the first launch of
+// jenga_forward_rotary.  As permute_pool_kernel (jenga_select.hip), a workgroup for a block of one (batch, head), tokens `token` elements
+// apart.  The turn is rounded to bf16 before it is stored and summed, so that the results are those of jenga_rotary and
+// jenga_forward one after the other.
+struct TurnedMoves {
+  const uint16_t* src[3];
+  Piece16* dst[3];
+  double* mean[2];
+  int64_t token;
+};
+template <int M_TOK, int D, bool HALVES>
+__global__ __launch_bounds__(256) void permute_turn_pool_kernel(TurnedMoves moves, Turns turns, const int32_t* __restrict__ src_of_pos,
+                                                                const int32_t* __restrict__ blk_valid, int n_src, int M_v, int batch) {
+  constexpr int CH = D / 8, G = 256 / CH, ROWS = M_TOK / G;   // pieces of a row, rows at a time, rows of a thread
+  __shared__ double red[G][D];
+  __shared__ __attribute__((aligned(16))) __bf16 room[HALVES ? 256 * 8 : 8];
+  const int h = blockIdx.x, j = blockIdx.y, heads = gridDim.x, M = gridDim.y;
+  const int tensor = blockIdx.z / batch, b = blockIdx.z - tensor * batch;
+  const int c = threadIdx.x % CH, g = threadIdx.x / CH;
+  const uint16_t* src = moves.src[tensor] + (size_t)b * n_src * moves.token + h * D + c * 8;
+  Piece16* dst = moves.dst[tensor] + (((size_t)b * heads + h) * M + j) * (M_TOK * CH) + threadIdx.x;
+  int s[ROWS];
+#pragma unroll
+  for (int u = 0; u < ROWS; ++u) s[u] = src_of_pos[j * M_TOK + u * G + g];
+  Piece16 v[ROWS];
+#pragma unroll
+  for (int u = 0; u < ROWS; ++u) {
+    v[u] = Piece16{{0, 0, 0, 0}};
+    if (s[u] >= 0) v[u] = *(const Piece16*)(src + (size_t)s[u] * moves.token);
+  }
+  if (tensor < 2 && j < M_v) {   // blocks of vision tokens hold no text
+    constexpr int N = HALVES ? 8 : 4;
+    Pair pair[N];
+    int other[N];
+    bool second[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) pair[i] = pair_of<HALVES>(turns, c * 8 + (HALVES ? i : 2 * i), &other[i], &second[i]);
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+      int cell[3] = {-1, -1, -1};
+      if (s[u] >= 0) turns.grid.split((uint32_t)s[u], cell);
+      f32x8 f = Eight<__bf16>::wide(v[u]);
+      float2 t;
+      if (HALVES) {
+        __builtin_memcpy(&room[threadIdx.x * 8], &v[u], 16);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // a row is 8 or 16 lanes of one wavefront
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float y = (float)room[g * D + other[i]];
+          if (turn_of(turns, pair[i], cell, &t)) f[i] = fmaf(f[i], t.x, second[i] ? y * t.y : -(y * t.y));
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float x = f[2 * i], y = f[2 * i + 1];
+          if (turn_of(turns, pair[i], cell, &t)) f[2 * i] = fmaf(x, t.x, -(y * t.y)), f[2 * i + 1] = fmaf(x, t.y, y * t.x);
+        }
+      }
+      v[u] = Eight<__bf16>::narrow(f);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < ROWS; ++u) dst[u * 256] = v[u];
+  if (tensor == 2 || (tensor == 0 && j >= M_v)) return;
+  double acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.0;
+#pragma unroll
+  for (int u = 0; u < ROWS; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc[2 * e] += bf16_bits_to_double(v[u].w[e] & 0xFFFFu);
+      acc[2 * e + 1] += bf16_bits_to_double(v[u].w[e] >> 16);
+    }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) red[g][c * 8 + e] = acc[e];
+  __syncthreads();
+  if (threadIdx.x < D) {
+    double sum = 0.0;
+#pragma unroll
+    for (int gg = 0; gg < G; ++gg) sum += red[gg][threadIdx.x];
+    const size_t row = ((size_t)b * heads + h) * (tensor == 0 ? M_v : M) + j;
+    moves.mean[tensor][row * D + pooled_pos<D>(j, threadIdx.x)] = sum / (double)blk_valid[j];
+  }
+}
+
+template <int M_TOK, int D>
+void run_permute_turn_pool(const jenga_plan* p, TurnedMoves moves, const Turns& turns, bool halves, void* ws, hipStream_t st) {
+  pooled_rows<D>(p, ws, &moves.mean[0], &moves.mean[1]);
+  const dim3 grid(p->cfg.heads, p->info.M, 3 * p->cfg.batch);
+  const int n_src = p->info.N_v + p->cfg.n_text;
+  if (halves)
+    permute_turn_pool_kernel<M_TOK, D, true><<<grid, 256, 0, st>>>(moves, turns, p->d_src_of_pos, p->d_blk_valid, n_src, p->info.M_v, p->cfg.batch);
+  else
+    permute_turn_pool_kernel<M_TOK, D, false><<<grid, 256, 0, st>>>(moves, turns, p->d_src_of_pos, p->d_blk_valid, n_src, p->info.M_v, p->cfg.batch);
+}
+
 }  // namespace
+
+namespace jenga {
+
+int launch_permute_turn_pool(const jenga_plan* p, const jenga_rotary_config& c, const float* table, const void* const src[3],
+                             int64_t token_stride, void* const dst[3], void* select_ws, void* stream) {
+  TurnedMoves moves = {{(const uint16_t*)src[0], (const uint16_t*)src[1], (const uint16_t*)src[2]},
+                       {(Piece16*)dst[0], (Piece16*)dst[1], (Piece16*)dst[2]}, {nullptr, nullptr}, token_stride};
+  const Turns turns = turns_of(c, table);
+  const bool halves = (c.flags & JENGA_ROTARY_HALVES) != 0;
+  hipStream_t st = (hipStream_t)stream;
+  const int m = p->cfg.block;
+  if (p->cfg.head_dim == 128) {
+    if (m == 128) run_permute_turn_pool<128, 128>(p, moves, turns, halves, select_ws, st);
+    else if (m == 64) run_permute_turn_pool<64, 128>(p, moves, turns, halves, select_ws, st);
+    else run_permute_turn_pool<32, 128>(p, moves, turns, halves, select_ws, st);
+  } else {
+    if (m == 128) run_permute_turn_pool<128, 64>(p, moves, turns, halves, select_ws, st);
+    else if (m == 64) run_permute_turn_pool<64, 64>(p, moves, turns, halves, select_ws, st);
+    else run_permute_turn_pool<32, 64>(p, moves, turns, halves, select_ws, st);
+  }
+  return status();
+}
+
+}  // namespace jenga
 
 extern "C" int jenga_rotary(const jenga_rotary_config* cfg, const jenga_plan* plan_or_null, const int32_t* cells_or_null,
                             const float* table, const jenga_rotary_tensor* tensors, int32_t count, int64_t batch, int64_t tokens,
@@ -140,21 +400,13 @@ extern "C" int jenga_rotary(const jenga_rotary_config* cfg, const jenga_plan* pl
     a.dst_head[k] = tensors[k].dst_head;
   }
   a.count = count;
-  a.table = (const float2*)table;
+  a.turns = turns_of(*cfg, table);
   a.cells = cells_or_null;
   a.src_of_pos = plan_or_null ? plan_or_null->d_src_of_pos : nullptr;
   a.tokens = tokens;
   a.units = batch * tokens;
-  a.grid = jenga::GridCells(cfg->T, cfg->H, cfg->W);
-  const int cells[3] = {cfg->T, cfg->H, cfg->W};
-  for (int i = 0, base = 0; i < 3; ++i) {
-    a.pairs[i] = cfg->dim[i] / 2;
-    a.base[i] = base;
-    base += cells[i] * a.pairs[i];
-  }
   a.head_dim = cfg->head_dim;
   a.heads_per_wg = 8;
-  a.sign = cfg->flags & JENGA_ROTARY_INVERSE ? -1.f : 1.f;
   const bool halves = (cfg->flags & JENGA_ROTARY_HALVES) != 0;
   hipStream_t st = (hipStream_t)stream;
   if (cfg->type == JENGA_BF16) return run_rotary<__bf16>(a, halves, st);

@@ -18,6 +18,7 @@
 #include <mutex>
 
 #include "jenga_internal.h"
+#include "jenga_pool.h"
 
 // Workspace of jenga_select_blocks_static: one copy per GPU, held from module load to process end.
 constexpr size_t STATIC_SCRATCH_BYTES = (size_t)JENGA_SELECT_STATIC_MAX_BYTES;
@@ -25,18 +26,9 @@ static __device__ __align__(256) unsigned char scratch[STATIC_SCRATCH_BYTES];
 
 namespace {
 
-__device__ inline double bf16_bits_to_double(uint32_t bits16) {
-  return (double)__uint_as_float(bits16 << 16);
-}
-
-// Where channel d of block j lies in its pooled row: pieces of 64 bytes, their order rotated by an exclusive or with the
-// block index.  select_kernel reads the same piece of 16 consecutive blocks at a time; without the rotation those lie
-// a row (1 KB at D = 128) apart and fall on a quarter of the L2's channels (the products of 929 x 931 blocks x 24 heads:
-// 175 us without it, 105 us with).
-template <int D>
-__device__ inline int pooled_pos(int j, int d) {
-  return ((((d >> 3) ^ j) & (D / 8 - 1)) << 3) | (d & 7);
-}
+using jenga::bf16_bits_to_double;
+using jenga::pooled_pos;
+using jenga::pooled_rows;
 
 // grid (M, batch*heads, 2): z = 0 pools Q (vision blocks only), z = 1 pools K (all blocks).
 // q, k: curve side [bh][n_pad][D]; qh: [bh][M_v][D]; kh: [bh][M][D].  A thread issues up to four row
@@ -581,14 +573,6 @@ __global__ __launch_bounds__(64 * ROWS, NT == 16 ? 1 : ROWS == 8 ? 4 : 8) void s
     return;
   }
   select_row<NT>(r, S[wave], fixed_lane, idx_out, mask_out, sel_count + out_row, M, K_top, p);
-}
-
-// Where the pooled rows of Q and K lie in the workspace.
-template <int D>
-void pooled_rows(const jenga_plan* p, void* ws, double** qh, double** kh) {
-  const size_t q_bytes = (size_t)p->cfg.batch * p->cfg.heads * p->info.M_v * D * 8;
-  *qh = (double*)ws;
-  *kh = (double*)((char*)ws + ((q_bytes + 255) & ~(size_t)255));
 }
 
 template <int D>
