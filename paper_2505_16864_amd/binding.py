@@ -228,52 +228,63 @@ def jenga_stage_switch(x_t, eps_t, eps_tilde, x_out, channels, in_shape, out_sha
 
 
 # The calls around the attention take torch tensors and read sizes, strides and types from them.  What the C ABI cannot see is
-# checked here: values next to each other in the last dimension, all tensors on the device that is current.
+# checked here: values next to each other in the last dimension, all tensors on the device that is current.  Small calls cost little
+# more than this code and a launch, so it is written without detours.
 
 _EINVAL = -1
+_TYPES = {}            # torch's element types to jenga_type, filled by the first call that needs them
+_DTYPE = {}            # and by name
+_current_device = None
 
 
-def _types():
+def _use_torch():
     import torch
-    return {torch.bfloat16: JENGA_BF16, torch.float16: JENGA_F16, torch.float32: JENGA_F32, torch.float8_e4m3fn: JENGA_E4M3,
-            torch.uint8: JENGA_E4M3}
+    global _current_device
+    _current_device = torch._C._cuda_getDevice
+    _DTYPE.update(f32=torch.float32, i32=torch.int32, u8=torch.uint8, bf16=torch.bfloat16, e4m3=torch.float8_e4m3fn)
+    _TYPES.update({torch.bfloat16: JENGA_BF16, torch.float16: JENGA_F16, torch.float32: JENGA_F32, torch.float8_e4m3fn: JENGA_E4M3,
+                   torch.uint8: JENGA_E4M3})
 
 
-_TYPES = {}
+def _refuse(what, why):
+    raise JengaError(_EINVAL, "%s: %s" % (what, why))
 
 
 def _type(t, what):
-    if not _TYPES:
-        _TYPES.update(_types())
     code = _TYPES.get(t.dtype)
     if code is None:
-        raise JengaError(_EINVAL, "%s: element type %s" % (what, t.dtype))
+        if not _TYPES:
+            _use_torch()
+            return _type(t, what)
+        _refuse(what, "element type %s" % t.dtype)
     return code
 
 
-def _need(ok, what, why):
-    if not ok:
-        raise JengaError(_EINVAL, "%s: %s" % (what, why))
+def _on_device(what, tensors):
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (t.get_device() != device or device < 0):
+            _refuse(what, "tensors are not all on one GPU")
+    if device != _current_device():
+        _refuse(what, "tensors are not on the current device")
 
 
-def _on_device(what, *tensors):
-    import torch
-    on = {t.get_device() for t in tensors if t is not None}
-    _need(len(on) == 1 and on != {-1} and on == {torch._C._cuda_getDevice()}, what, "a tensor is not on the current device")
-
-
-def _matrix(t, what, shape=None):
+def _matrix(t, what, rows=None, cols=None):
     """The row stride of a matrix; of a single row any stride will do."""
-    _need(t.dim() == 2 and (shape is None or tuple(t.shape) == tuple(shape)), what, "shape %s" % (tuple(t.shape),))
-    _need(t.stride(1) == 1 or t.shape[1] == 1, what, "values of a row are not next to each other")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and (shape[0] != rows or shape[1] != cols)):
+        _refuse(what, "shape %s" % (tuple(shape),))
+    stride = t.stride()
+    if stride[1] != 1 and shape[1] != 1:
+        _refuse(what, "values of a row are not next to each other")
+    return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
 
 
-def _plain(t, what, shape, dtype):
-    """A tensor of this shape and type without gaps, or None."""
-    if t is not None:
-        _need(tuple(t.shape) == tuple(shape) and str(t.dtype)[6:] in dtype and t.is_contiguous(), what,
-              "shape %s, type %s" % (tuple(t.shape), t.dtype))
+def _whole(t, what, shape, dtype):
+    """Refuses anything but a tensor of this shape and type (a name in _DTYPE) without gaps."""
+    if t.shape != shape or t.dtype != _DTYPE[dtype] or not t.is_contiguous():
+        if dtype != "e4m3" or t.dtype != _DTYPE["u8"] or t.shape != shape or not t.is_contiguous():   # its bytes will do
+            _refuse(what, "shape %s, type %s" % (tuple(t.shape), t.dtype))
 
 
 def scale_columns(cols):
@@ -286,53 +297,57 @@ def padded_columns(cols):
     return -(-cols // 128) * 128
 
 
-_E4M3 = ("float8_e4m3fn", "uint8")
-
-
 def jenga_quantize(x, q, scale, block_rows=1, stream=None):
     """x [rows, cols] -> q e4m3 [rows, padded_columns(cols)], scale uint8 [rows or ceil(rows / 128), scale_columns(cols)]."""
     what = "jenga_quantize"
-    stride = _matrix(x, what)
+    stride, kind = _matrix(x, what), _type(x, what)
     rows, cols = x.shape
-    _plain(q, what, (rows, padded_columns(cols)), _E4M3)
-    _need(block_rows in (1, 128), what, "blocks of %s rows" % block_rows)
-    _plain(scale, what, (-(-rows // block_rows), scale_columns(cols)), ("uint8",))
-    _on_device(what, x, q, scale)
-    if rows == 0:
-        return
-    _check(_lib.jenga_quantize(_ptr(x), stride, _type(x, what), rows, cols, block_rows, _ptr(q), _ptr(scale), stream), what)
+    if block_rows not in (1, 128):
+        _refuse(what, "blocks of %s rows" % block_rows)
+    _whole(q, what, (rows, padded_columns(cols)), "e4m3")
+    _whole(scale, what, (-(-rows // block_rows), scale_columns(cols)), "u8")
+    _on_device(what, (x, q, scale))
+    if rows:
+        _check(_lib.jenga_quantize(x.data_ptr(), stride, kind, rows, cols, block_rows, q.data_ptr(), scale.data_ptr(), stream), what)
 
 
 def jenga_matmul(a, a_scale, b, b_scale, out, bias=None, stream=None):
     """out [m, n] = a b^T + bias for 8-bit tensors a [m, k] (blocks of 1 x 128) and b [n, k] (128 x 128); bias float32 [n]."""
     what = "jenga_matmul"
-    stride = _matrix(out, what, (a.shape[0], b.shape[0]))
-    (m, n), k = out.shape, a.shape[1]
-    _plain(a, what, (m, k), _E4M3)
-    _plain(b, what, (n, k), _E4M3)
-    _plain(a_scale, what, (m, scale_columns(k)), ("uint8",))
-    _plain(b_scale, what, (-(-n // 128), scale_columns(k)), ("uint8",))
-    _plain(bias, what, (n,), ("float32",))
-    _on_device(what, a, a_scale, b, b_scale, out, bias)
-    if m == 0:
-        return
-    cfg = jenga_matmul_config(m, stride, n, k, _type(out, what), 0)
-    _check(_lib.jenga_matmul(ctypes.byref(cfg), _ptr(a), _ptr(a_scale), _ptr(b), _ptr(b_scale), _ptr(bias), _ptr(out), stream), what)
+    (m, k), n, kind = a.shape, b.shape[0], _type(out, what)
+    stride = _matrix(out, what, m, n)
+    scales = scale_columns(k)
+    _whole(a, what, (m, k), "e4m3")
+    _whole(b, what, (n, k), "e4m3")
+    _whole(a_scale, what, (m, scales), "u8")
+    _whole(b_scale, what, (-(-n // 128), scales), "u8")
+    if bias is not None:
+        _whole(bias, what, (n,), "f32")
+    _on_device(what, (a, a_scale, b, b_scale, out, bias))
+    if m:
+        _check(_lib.jenga_matmul(ctypes.byref(jenga_matmul_config(m, stride, n, k, kind, 0)), a.data_ptr(), a_scale.data_ptr(),
+                                 b.data_ptr(), b_scale.data_ptr(), None if bias is None else bias.data_ptr(), out.data_ptr(), stream), what)
 
 
 def _norm_config(what, x, y, weight, bias, group_rows, weight_offset, eps):
-    x_stride = _matrix(x, what)
+    x_stride, x_type, y_type = _matrix(x, what), _type(x, what), _type(y, what)
     rows, cols = x.shape
-    group_rows = group_rows or max(rows, 1)
-    _need(group_rows > 0, what, "groups of %d rows" % group_rows)
-    groups = -(-rows // group_rows)
-    params = [(p.unsqueeze(0) if p.dim() == 1 else p) for p in (weight, bias) if p is not None]
-    strides = [_matrix(p, what, (groups, cols) if rows else None) for p in params]
-    _need(len(set(strides)) < 2 and len({p.dtype for p in params}) < 2, what, "weight and bias differ in stride or type")
-    e4m3 = _type(y, what) == JENGA_E4M3
-    y_stride = _matrix(y, what, (rows, padded_columns(cols) if e4m3 else cols))
-    return jenga_norm_config(rows, group_rows, x_stride, y_stride, strides[0] if strides else cols, cols, _type(x, what),
-                             _type(y, what), _type(params[0], what) if params else JENGA_F32, eps, weight_offset)
+    if group_rows < 0:
+        _refuse(what, "groups of %d rows" % group_rows)
+    group_rows = group_rows or rows or 1
+    param_stride, param_type = cols, x_type
+    for p in (bias, weight):
+        if p is not None:
+            shape, stride = p.shape, p.stride()
+            groups = -(-rows // group_rows)
+            if shape[-1] != cols or stride[-1] != 1 and cols != 1 or len(shape) > 2 or (rows and (shape[0] if len(shape) == 2 else 1) != groups):
+                _refuse(what, "weight or bias of shape %s" % (tuple(shape),))
+            stride = stride[0] if groups > 1 else cols
+            if p is weight and bias is not None and (stride != param_stride or p.dtype != bias.dtype):
+                _refuse(what, "weight and bias differ in stride or type")
+            param_stride, param_type = stride, _type(p, what)
+    y_stride = _matrix(y, what, rows, cols if y_type != JENGA_E4M3 else padded_columns(cols))
+    return jenga_norm_config(rows, group_rows, x_stride, y_stride, param_stride, cols, x_type, y_type, param_type, eps, weight_offset)
 
 
 def jenga_layer_norm(x, y, weight=None, bias=None, y_scale=None, mean=None, rstd=None, group_rows=0, weight_offset=0.0,
@@ -341,14 +356,19 @@ def jenga_layer_norm(x, y, weight=None, bias=None, y_scale=None, mean=None, rstd
     float32 [rows].  y in e4m3: [rows, padded_columns(cols)] with y_scale uint8 [rows, scale_columns(cols)]."""
     what = "jenga_layer_norm"
     cfg = _norm_config(what, x, y, weight, bias, group_rows, weight_offset, eps)
-    _plain(y_scale, what, (cfg.rows, scale_columns(cfg.cols)), ("uint8",))
-    _plain(mean, what, (cfg.rows,), ("float32",))
-    _plain(rstd, what, (cfg.rows,), ("float32",))
-    _on_device(what, x, y, weight, bias, y_scale, mean, rstd)
-    if cfg.rows == 0:
-        return
-    _check(_lib.jenga_layer_norm(ctypes.byref(cfg), _ptr(x), _ptr(weight), _ptr(bias), _ptr(y), _ptr(y_scale), _ptr(mean),
-                                 _ptr(rstd), stream), what)
+    rows, cols = x.shape
+    if y_scale is not None:
+        _whole(y_scale, what, (rows, scale_columns(cols)), "u8")
+    if mean is not None:
+        _whole(mean, what, (rows,), "f32")
+    if rstd is not None:
+        _whole(rstd, what, (rows,), "f32")
+    _on_device(what, (x, y, weight, bias, y_scale, mean, rstd))
+    if rows:
+        _check(_lib.jenga_layer_norm(ctypes.byref(cfg), x.data_ptr(), None if weight is None else weight.data_ptr(),
+                                     None if bias is None else bias.data_ptr(), y.data_ptr(),
+                                     None if y_scale is None else y_scale.data_ptr(), None if mean is None else mean.data_ptr(),
+                                     None if rstd is None else rstd.data_ptr(), stream), what)
 
 
 def jenga_layer_norm_grad_workspace(rows, cols, group_rows=0):
@@ -364,21 +384,24 @@ def jenga_layer_norm_grad(x, dy, dx, weight, mean, rstd, dweight=None, dbias=Non
     """Gradients of x [rows, cols] and of weight and bias, float32 [groups, cols], from dy and jenga_layer_norm's mean and rstd."""
     what = "jenga_layer_norm_grad"
     cfg = _norm_config(what, x, dy, weight, None, group_rows, weight_offset, 0.0)
-    _need(cfg.y_type == cfg.x_type, what, "dy is not of x's type")
-    _need(_matrix(dx, what, x.shape) == cfg.x_stride and dx.dtype == x.dtype, what, "dx is not laid out as x is")
-    groups = -(-cfg.rows // cfg.group_rows)
-    for t in (mean, rstd):
-        _need(t is not None, what, "mean and rstd of the forward pass are wanted")
-        _plain(t, what, (cfg.rows,), ("float32",))
+    rows, cols = x.shape
+    if cfg.y_type != cfg.x_type or dx.dtype != x.dtype or _matrix(dx, what, rows, cols) != cfg.x_stride:
+        _refuse(what, "dy is not of x's type, or dx is not laid out as x is")
+    if mean is None or rstd is None:
+        _refuse(what, "mean and rstd of the forward pass are wanted")
+    _whole(mean, what, (rows,), "f32")
+    _whole(rstd, what, (rows,), "f32")
+    groups = -(-rows // cfg.group_rows)
     for t in (dweight, dbias):
-        _need(t is None or t.numel() == groups * cfg.cols, what, "gradients of %d groups" % groups)
-        _plain(t, what, t.shape if t is not None else (), ("float32",))
-    _on_device(what, x, dy, dx, weight, mean, rstd, dweight, dbias, workspace)
-    if cfg.rows == 0:
-        return
-    room = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(_lib.jenga_layer_norm_grad(ctypes.byref(cfg), _ptr(x), _ptr(dy), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dx),
-                                      _ptr(dweight), _ptr(dbias), _ptr(workspace), room, stream), what)
+        if t is not None:
+            if t.numel() != groups * cols:
+                _refuse(what, "gradients of %d groups" % groups)
+            _whole(t, what, t.shape, "f32")
+    _on_device(what, (x, dy, dx, weight, mean, rstd, dweight, dbias, workspace))
+    if rows:
+        _check(_lib.jenga_layer_norm_grad(ctypes.byref(cfg), x.data_ptr(), dy.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(),
+                                          dx.data_ptr(), _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                                          0 if workspace is None else workspace.numel() * workspace.element_size(), stream), what)
 
 
 def make_rotary(T, H, W, head_dim, dims, theta=10000.0, origin=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0), flags=0):
@@ -392,39 +415,47 @@ def jenga_rotary_table(cfg, table):
     want = cfg.T * cfg.dim[0] + cfg.H * cfg.dim[1] + cfg.W * cfg.dim[2]
     count = table.numel() if hasattr(table, "numel") else table.size
     contiguous = table.is_contiguous() if hasattr(table, "is_contiguous") else table.flags.c_contiguous
-    _need(count == want and str(table.dtype).endswith("float32") and contiguous and not getattr(table, "is_cuda", False),
-          "jenga_rotary_table", "a table of %d float32 on the host is wanted" % want)
+    if count != want or not str(table.dtype).endswith("float32") or not contiguous or getattr(table, "is_cuda", False):
+        _refuse("jenga_rotary_table", "a table of %d float32 on the host is wanted" % want)
     _check(_lib.jenga_rotary_table(ctypes.byref(cfg), _ptr(table)), "jenga_rotary_table")
 
 
 def _rotary_table(cfg, table, what):
-    _need(table.numel() == cfg.T * cfg.dim[0] + cfg.H * cfg.dim[1] + cfg.W * cfg.dim[2] and table.is_contiguous() and
-          str(table.dtype).endswith("float32"), what, "not a table of this grid")
+    dim = cfg.dim
+    if table.numel() != cfg.T * dim[0] + cfg.H * dim[1] + cfg.W * dim[2] or not table.is_contiguous() or _type(table, what) != JENGA_F32:
+        _refuse(what, "not a table of this grid")
+
+
+def _rotary_tensor(cfg, src, dst, what):
+    shape, s, d = src.shape, src.stride(), dst.stride()
+    if len(shape) != 4 or dst.shape != shape or shape[3] != cfg.head_dim:
+        _refuse(what, "shapes %s, %s" % (tuple(shape), tuple(dst.shape)))
+    if s[3] != 1 or d[3] != 1 or dst.dtype != src.dtype:
+        _refuse(what, "types differ or the channels of a head are not next to each other")
+    return jenga_rotary_tensor(src.data_ptr(), dst.data_ptr(), s[0], s[1], s[2], d[0], d[1], d[2], shape[2], 0)
 
 
 def jenga_rotary(cfg, table, q, q_out, k=None, k_out=None, cells=None, plan=None, stream=None):
     """q, k [batch, tokens, heads, head_dim] (heads may differ, any strides but the last) -> q_out, k_out, which may be q and k.
     plan: tokens in its curve order (a curve-side tensor transposed to this shape); cells: int32 [batch, tokens, 3]."""
     what = "jenga_rotary"
-    batch, tokens = q.shape[:2]
-    tensors = (jenga_rotary_tensor * 2)()
-    pairs = [(q, q_out)] if k is None else [(q, q_out), (k, k_out)]
-    for t, (src, dst) in zip(tensors, pairs):
-        _need(src.dim() == 4 and src.shape == dst.shape and src.shape[:2] == q.shape[:2] and src.shape[3] == cfg.head_dim, what,
-              "shapes %s, %s" % (tuple(src.shape), tuple(dst.shape)))
-        _need(src.dtype == q.dtype and dst.dtype == q.dtype and src.stride(3) == 1 and dst.stride(3) == 1, what,
-              "types differ or the channels of a head are not next to each other")
-        t.src, t.dst, t.heads = src.data_ptr(), dst.data_ptr(), src.shape[2]
-        t.src_batch, t.src_token, t.src_head = src.stride()[:3]
-        t.dst_batch, t.dst_token, t.dst_head = dst.stride()[:3]
+    kind = _type(q, what)
+    if k is None:
+        tensors = (jenga_rotary_tensor * 1)(_rotary_tensor(cfg, q, q_out, what))
+    else:
+        tensors = (jenga_rotary_tensor * 2)(_rotary_tensor(cfg, q, q_out, what), _rotary_tensor(cfg, k, k_out, what))
+        if k.dtype != q.dtype or k.shape[:2] != q.shape[:2]:
+            _refuse(what, "q and k differ in type or tokens")
+    batch, tokens = q.shape[0], q.shape[1]
     _rotary_table(cfg, table, what)
-    _plain(cells, what, (batch, tokens, 3), ("int32",))
-    _on_device(what, table, q, q_out, k, k_out, cells)
-    if batch == 0 or tokens == 0:
-        return
-    mine = jenga_rotary_config.from_buffer_copy(cfg)
-    mine.type = _type(q, what)
-    _check(_lib.jenga_rotary(ctypes.byref(mine), plan, _ptr(cells), _ptr(table), tensors, len(pairs), batch, tokens, stream), what)
+    if cells is not None:
+        _whole(cells, what, (batch, tokens, 3), "i32")
+    _on_device(what, (q, q_out, k, k_out, table, cells))
+    if batch and tokens:
+        mine = jenga_rotary_config.from_buffer_copy(cfg)
+        mine.type = kind
+        _check(_lib.jenga_rotary(ctypes.byref(mine), plan, None if cells is None else cells.data_ptr(), table.data_ptr(), tensors,
+                                 len(tensors), batch, tokens, stream), what)
 
 
 def jenga_forward_rotary(plan, cfg, table, q_thw, k_thw, v_thw, q_curve, k_curve, v_curve, sel_count, sel_index, mask,
@@ -435,11 +466,12 @@ def jenga_forward_rotary(plan, cfg, table, q_thw, k_thw, v_thw, q_curve, k_curve
     batch, tokens, heads, dim = q_thw.shape
     stride = q_thw.stride(1) if tokens > 1 else q_thw.stride(0) if batch > 1 else heads * dim
     for t in (q_thw, k_thw, v_thw):
-        _need(t.shape == q_thw.shape and str(t.dtype) == "torch.bfloat16" and t.stride(3) == 1 and (heads == 1 or t.stride(2) == dim) and
-              (tokens == 1 or t.stride(1) == stride) and (batch == 1 or t.stride(0) == stride * tokens), what,
-              "shape %s, strides %s" % (tuple(t.shape), t.stride()))
+        s = t.stride()
+        if t.shape != q_thw.shape or _type(t, what) != JENGA_BF16 or s[3] != 1 or (heads > 1 and s[2] != dim) or \
+                (tokens > 1 and s[1] != stride) or (batch > 1 and s[0] != stride * tokens):
+            _refuse(what, "shape %s, strides %s, type %s" % (tuple(t.shape), s, t.dtype))
     _rotary_table(cfg, table, what)
-    _on_device(what, table, q_thw, k_thw, v_thw)
+    _on_device(what, (table, q_thw, k_thw, v_thw))
     _check(_lib.jenga_forward_rotary(plan, ctypes.byref(cfg), _ptr(table), _ptr(q_thw), _ptr(k_thw), _ptr(v_thw), stride, _ptr(q_curve),
                                      _ptr(k_curve), _ptr(v_curve), _ptr(sel_count), _ptr(sel_index), _ptr(mask),
                                      _ptr(select_workspace), select_workspace_bytes, _ptr(out_curve), _ptr(lse),

@@ -160,7 +160,6 @@ int norm_grad_args_ok(const jenga_norm_config* c, const void* x, const void* dy,
   if (dweight || dbias) {
     if (!workspace || !aligned(workspace, 256)) return JENGA_EINVAL;
     need = (uint64_t)(1024 + groups) * c->cols * 8;
-    if (workspace_bytes < need) return JENGA_EWORKSPACE;
   }
   const int64_t width = (int64_t)c->cols * xs, sums = groups * c->cols * 4;
   const Span in[5] = {{x, c->rows, c->x_stride * xs, width}, {dy, c->rows, c->y_stride * xs, width},
@@ -174,12 +173,7 @@ int norm_grad_args_ok(const jenga_norm_config* c, const void* x, const void* dy,
     for (int j = 0; j < i; ++j)
       if (overlap(out[i], out[j])) return JENGA_EINVAL;
   }
-  return JENGA_OK;
-}
-
-int norm_grad_parts(const jenga_norm_config& c) {
-  const int64_t groups = groups_of(c), rows = std::min(c.rows, c.group_rows);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(512 / groups, (rows + 7) / 8));
+  return workspace_bytes < need ? JENGA_EWORKSPACE : JENGA_OK;
 }
 
 int quantize_args_ok(const void* x, int64_t x_stride, int32_t x_type, int64_t rows, int32_t cols, int32_t block_rows, const void* q,

@@ -204,9 +204,6 @@ int rotary_config_ok(const jenga_rotary_config* c);
 int rotary_args_ok(const jenga_rotary_config* c, const jenga_plan* plan, const int32_t* cells, const float* table,
                    const jenga_rotary_tensor* tensors, int32_t count, int64_t batch, int64_t tokens);
 
-// Workgroups that share the rows of a group in the gradient of the norm.
-int norm_grad_parts(const jenga_norm_config& c);
-
 // Kernel launchers (defined in the .hip files).  All return a jenga_status.
 // 1 to 3 tensors of the plan's shape
 int launch_permute(const jenga_plan* p, const void* const* src, void* const* dst, int tensors, bool forward,

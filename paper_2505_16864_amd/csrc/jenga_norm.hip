@@ -55,52 +55,134 @@ __device__ __forceinline__ void put(const NormArgs& a, int64_t row, int col, con
   if ((threadIdx.x & 15) == 0 && block < a.scale_cols) a.y_scale[row * a.scale_cols + block] = block < blocks ? (uint8_t)byte : 0;
 }
 
-// A wavefront per row, up to NV pieces of 512 columns.
+// Rows in registers are taken in pieces of eight columns.  Where their number is no multiple of eight, the last piece ends with the row
+// and overlaps the one before it: both compute and store the same results there, and the sums take only what is `own`.  (Columns one
+// by one at the end of a row cost a branch each in every piece: 33272 x 5120 bf16 177 us.)  E4M3 results have their places in
+// blocks, so there it has to be a multiple of eight.
+struct Piece {
+  int col;     // of the first value; 8 of them
+  int skip;    // so many are the piece's before
+  bool here;
+};
+__device__ __forceinline__ Piece piece_at(int col, int cols) {
+  const int c = min(col, cols - 8);
+  return {c, col - c, col < cols};
+}
+template <typename T>
+__device__ __forceinline__ typename Eight<T>::raw take(const T* p, bool here) {
+  typename Eight<T>::raw r = {};
+  if (here) r = *(const typename Eight<T>::raw*)p;
+  return r;
+}
+
+// Sum over the WPR wavefronts of a row; all of them get it.  `room` is not written again before everybody has read it.
+template <int WPR>
+__device__ __forceinline__ float row_sum(float v, float* room) {
+  v = wave_sum_f32(v);
+  if (WPR == 1) return v;
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) room[wave] = v;
+  __syncthreads();
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < WPR; ++i) s += room[wave / WPR * WPR + i];
+  return s;
+}
+
+// Workgroups of norm_kernel on a compute unit, by the registers that it needs.  The grid is as many and no more: with 8 a CU
+// where 5 have room, the last ones run on a chip that is half empty.
 template <typename X, typename P, bool E4M3, int NV>
-__global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.rows; row += (int64_t)gridDim.x * 4) {
+constexpr int norm_per_cu() {
+  constexpr bool HALF = sizeof(X) + sizeof(P) == 4;   // both of 16 bits
+  return NV == 1 ? (HALF ? 8 : 6) : NV == 2 ? (HALF && !E4M3 ? 5 : 4) : NV == 3 ? (HALF ? (E4M3 ? 4 : 5) : 3) : HALF ? 3 : 2;
+}
+
+// WPR wavefronts to a row, up to NV pieces of WPR * 512 columns, cols >= 8.  A workgroup takes rows a grid apart; it keeps the weight and the
+// bias in registers, and the next row is on its way while one is worked on.  (A wavefront alone with 80 columns a lane: 33272 x
+// 5120 bf16 177 us.)
+template <typename X, typename P, bool E4M3, int NV, int WPR>
+__global__ __launch_bounds__(256, (norm_per_cu<X, P, E4M3, NV>())) void norm_kernel(NormArgs a) {
+  constexpr int STEP = WPR * 512, AT_ONCE = 4 / WPR;
+  __shared__ float room[2][2][4];
+  const int slot = (threadIdx.x >> 6) / WPR, col0 = (threadIdx.x % (WPR * 64)) * 8;
+  typename Eight<P>::raw weight[NV], bias[NV];
+  int64_t have = -1;   // whose group's they are
+  typename Eight<X>::raw next[NV];
+  auto fetch = [&](int64_t row) {   // zeros for a row that is not there
     const X* x = (const X*)a.x + row * a.x_stride;
-    typename Eight<X>::raw raw[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+      if (v * STEP < a.cols) {
+        const Piece p = piece_at(v * STEP + col0, a.cols);
+        next[v] = take(x + p.col, p.here && row < a.rows);
+      }
+  };
+  const int64_t step = (int64_t)gridDim.x * AT_ONCE;
+  fetch((int64_t)blockIdx.x * AT_ONCE + slot);
+  int turn = 0;
+  // every wavefront takes every turn (there are barriers in it); one without a row has zeros and nothing to store
+  for (int64_t row0 = (int64_t)blockIdx.x * AT_ONCE; row0 < a.rows; row0 += step, turn ^= 1) {
+    const int64_t row = row0 + slot;
+    const bool mine = row < a.rows;
+    const int64_t group = a.rows > a.group_rows && mine ? row / a.group_rows : 0;
+    if (group != have) {
+      have = group;
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        if (v * STEP < a.cols) {
+          const Piece p = piece_at(v * STEP + col0, a.cols);
+          weight[v] = take((const P*)a.weight + group * a.param_stride + p.col, p.here && a.weight);
+          bias[v] = take((const P*)a.bias + group * a.param_stride + p.col, p.here && a.bias);
+        }
+    }
+    f32x8 f[NV];   // x, then x - mean
     float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
-      if (v * 512 < a.cols) raw[v] = load_eight(x + v * 512 + lane * 8, a.cols - v * 512 - lane * 8);
+      if (v * STEP < a.cols) {
+        f[v] = Eight<X>::wide(next[v]);
+        if (v * STEP + STEP <= a.cols) {
+          sum += ((f[v][0] + f[v][1]) + (f[v][2] + f[v][3])) + ((f[v][4] + f[v][5]) + (f[v][6] + f[v][7]));
+        } else {
+          const Piece p = piece_at(v * STEP + col0, a.cols);
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      if (v * 512 < a.cols) {
-        const f32x8 f = Eight<X>::wide(raw[v]);
-        sum += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+          for (int i = 0; i < 8; ++i) sum += i >= p.skip ? f[v][i] : 0.f;   // zeros where there is no piece
+        }
       }
-    const float mean = wave_sum_f32(sum) / (float)a.cols;
+    fetch(row + step);
+    const float mean = row_sum<WPR>(sum, room[turn][0]) / (float)a.cols;
     float square = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
-      if (v * 512 < a.cols) {
-        const f32x8 f = Eight<X>::wide(raw[v]);
+      if (v * STEP < a.cols) {
+        f[v] -= mean;
+        if (v * STEP + STEP <= a.cols) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float d = f[i] - mean;
-          if (v * 512 + lane * 8 + i < a.cols) square = fmaf(d, d, square);
+          for (int i = 0; i < 8; ++i) square = fmaf(f[v][i], f[v][i], square);
+        } else {
+          const Piece p = piece_at(v * STEP + col0, a.cols);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) square = fmaf(f[v][i], p.here && i >= p.skip ? f[v][i] : 0.f, square);
         }
       }
-    const float rstd = 1.0f / sqrtf(wave_sum_f32(square) / (float)a.cols + a.eps);
-    if (lane == 0) {
+    const float rstd = 1.0f / sqrtf(row_sum<WPR>(square, room[turn][1]) / (float)a.cols + a.eps);
+    if (mine && threadIdx.x % (WPR * 64) == 0) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
-    const int64_t group = row / a.group_rows;
+    if (mine) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-      if (v * 512 < a.cols) {
-        const int col = v * 512 + lane * 8;
-        const f32x8 f = Eight<X>::wide(raw[v]);
-        f32x8 w, b, y;
-        params<P>(a, group, col, &w, &b);
+      for (int v = 0; v < NV; ++v)
+        if (v * STEP < a.cols) {
+          const Piece p = piece_at(v * STEP + col0, a.cols);
+          const f32x8 w = Eight<P>::wide(weight[v]) + a.w0, b = Eight<P>::wide(bias[v]);
+          f32x8 y;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = fmaf((f[i] - mean) * rstd, w[i], b[i]);
-        put<X, E4M3>(a, row, col, y);
-      }
+          for (int i = 0; i < 8; ++i) y[i] = fmaf(f[v][i] * rstd, w[i], b[i]);
+          if (E4M3) put<X, true>(a, row, v * STEP + col0, y);
+          else if (p.here) *(typename Eight<X>::raw*)((X*)a.y + row * a.y_stride + p.col) = Eight<X>::narrow(y);
+        }
+    }
   }
 }
 
@@ -165,12 +247,19 @@ __device__ __forceinline__ void part_rows(const NormArgs& a, int64_t group, int 
   *end = start + n * (part + 1) / a.row_parts;
 }
 
-// A workgroup takes a part of a group's rows, WPR wavefronts to a row, up to NV pieces of WPR * 512 columns, and keeps the sums of
-// its columns in registers; they go to parts[workgroup][2][cols].
+// Wavefronts of norm_grad_kernel on a SIMD, by the registers that it needs.
+template <int NV>
+constexpr int grad_per_cu() {
+  return NV == 1 ? 4 : NV == 2 ? 3 : 2;
+}
+
+// A workgroup takes a part of a group's rows, WPR wavefronts to a row, up to NV pieces of WPR * 512 columns, and keeps the weight and
+// the sums of its columns in registers; the sums go to parts[workgroup][2][cols].  The next row is on its way while one is worked on.
+constexpr int grad_waves(int wpr) { return wpr > 4 ? wpr : 4; }
 template <typename X, typename P, int NV, int WPR>
-__global__ __launch_bounds__(256) void norm_grad_kernel(NormArgs a) {
-  constexpr int STEP = WPR * 512, AT_ONCE = 4 / WPR;
-  __shared__ float room[2][4][2];
+__global__ __launch_bounds__(64 * grad_waves(WPR), (grad_per_cu<NV>())) void norm_grad_kernel(NormArgs a) {
+  constexpr int STEP = WPR * 512, WAVES = grad_waves(WPR), AT_ONCE = WAVES / WPR;
+  __shared__ float room[2][WAVES][2];
   extern __shared__ float sums[];   // [2][cols], for the rows of AT_ONCE wavefronts
   const int64_t group = blockIdx.x / a.row_parts;
   const int part = blockIdx.x - (int)(group * a.row_parts);
@@ -179,36 +268,53 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(NormArgs a) {
   int64_t first, end;
   part_rows(a, group, part, &first, &end);
   f32x8 dw[NV], db[NV];
+  typename Eight<P>::raw weight[NV];
 #pragma unroll
-  for (int v = 0; v < NV; ++v) dw[v] = db[v] = 0.f;
+  for (int v = 0; v < NV; ++v) {
+    dw[v] = db[v] = 0.f;
+    const Piece p = piece_at(v * STEP + col0, a.cols);
+    if (a.weight) weight[v] = take((const P*)a.weight + group * a.param_stride + p.col, p.here);
+  }
+  typename Eight<X>::raw next_x[NV], next_d[NV];
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto fetch = [&](int64_t row) {   // zeros for a row that is not there
+    const X *x = (const X*)a.x + row * a.x_stride, *dy = (const X*)a.dy + row * a.y_stride;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+      if (v * STEP < a.cols) {
+        const Piece p = piece_at(v * STEP + col0, a.cols);
+        next_x[v] = take(x + p.col, p.here && row < end);
+        next_d[v] = take(dy + p.col, p.here && row < end);
+      }
+    if (row < end) next_mean = a.mean[row], next_rstd = a.rstd[row];
+  };
+  fetch(first + slot);
   int turn = 0;
-  // every wavefront takes every turn (there are barriers in it); one without a row has nothing to store
+  // every wavefront takes every turn (there are barriers in it); one without a row has zeros and nothing to store
   for (int64_t row0 = first; row0 < end; row0 += AT_ONCE, turn ^= 1) {
     const int64_t row = row0 + slot;
-    const bool mine = row < end;
+    const float mean = next_mean, rstd = next_rstd;
     f32x8 h[NV], g[NV];
-    float rstd = 0.f, mean = 0.f, sum_g = 0.f, sum_gh = 0.f;
-    if (mine) mean = a.mean[row], rstd = a.rstd[row];
+    float sum_g = 0.f, sum_gh = 0.f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      h[v] = g[v] = 0.f;
-      const int col = v * STEP + col0, n = a.cols - col;
-      if (mine && n > 0) {
+    for (int v = 0; v < NV; ++v)
+      if (v * STEP < a.cols) {
+        const f32x8 x = Eight<X>::wide(next_x[v]), d = Eight<X>::wide(next_d[v]);
         f32x8 w = a.w0;
-        if (a.weight) w += Eight<P>::wide(load_eight((const P*)a.weight + group * a.param_stride + col, n));
-        const f32x8 x = Eight<X>::wide(load_eight((const X*)a.x + row * a.x_stride + col, n));
-        const f32x8 d = Eight<X>::wide(load_eight((const X*)a.dy + row * a.y_stride + col, n));
+        if (a.weight) w += Eight<P>::wide(weight[v]);
+        const int skip = v * STEP + STEP <= a.cols ? 0 : piece_at(v * STEP + col0, a.cols).skip;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          h[v][i] = i < n ? (x[i] - mean) * rstd : 0.f;
-          g[v][i] = d[i] * w[i];   // d is 0 past the end
+          h[v][i] = (x[i] - mean) * rstd;
+          g[v][i] = d[i] * w[i];   // 0 where there is no piece
           dw[v][i] = fmaf(d[i], h[v][i], dw[v][i]);
           db[v][i] += d[i];
-          sum_g += g[v][i];
-          sum_gh = fmaf(g[v][i], h[v][i], sum_gh);
+          const float own = i >= skip ? g[v][i] : 0.f;
+          sum_g += own;
+          sum_gh = fmaf(own, h[v][i], sum_gh);
         }
       }
-    }
+    fetch(row + AT_ONCE);
     sum_g = wave_sum_f32(sum_g);
     sum_gh = wave_sum_f32(sum_gh);
     if (WPR > 1) {
@@ -220,15 +326,14 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(NormArgs a) {
     }
     const float mg = sum_g / (float)a.cols, mgh = sum_gh / (float)a.cols;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int col = v * STEP + col0, n = a.cols - col;
-      if (mine && n > 0) {
+    for (int v = 0; v < NV; ++v)
+      if (v * STEP < a.cols) {
+        const Piece p = piece_at(v * STEP + col0, a.cols);
         f32x8 d;
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = rstd * (g[v][i] - mg - h[v][i] * mgh);
-        store_eight((X*)a.dx + row * a.x_stride + col, d, n);
+        if (p.here && row < end) *(typename Eight<X>::raw*)((X*)a.dx + row * a.x_stride + p.col) = Eight<X>::narrow(d);
       }
-    }
   }
   if (!a.parts) return;
   float* to = a.parts + (int64_t)blockIdx.x * 2 * a.cols;
@@ -238,8 +343,9 @@ __global__ __launch_bounds__(256) void norm_grad_kernel(NormArgs a) {
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int col = v * STEP + col0 + i;
-          if (col < a.cols) {
+          const Piece p = piece_at(v * STEP + col0, a.cols);
+          const int col = p.col + i;
+          if (p.here && i >= p.skip) {
             float w = dw[v][i], b = db[v][i];
             if (s > 0) w += sums[col], b += sums[a.cols + col];
             if (s == AT_ONCE - 1) to[col] = w, to[a.cols + col] = b;
@@ -299,19 +405,24 @@ __global__ __launch_bounds__(256) void norm_grad_columns_kernel(NormArgs a) {
   to[a.cols + col] = db;
 }
 
-// Adds up the parts of each group, in order: 64 columns a workgroup, four of its wavefronts a quarter of the parts each.
-__global__ __launch_bounds__(256) void norm_grad_sum_kernel(const float* __restrict__ parts, float* __restrict__ dweight,
-                                                            float* __restrict__ dbias, int cols, int row_parts) {
-  __shared__ float room[4][64];
-  const int c = blockIdx.y * 64 + (threadIdx.x & 63), quarter = threadIdx.x >> 6;   // column of [2][cols]
+// Adds up the parts of each group: 64 columns a workgroup, sixteen wavefronts a sixteenth of the parts each, in order.
+__global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* __restrict__ parts, float* __restrict__ dweight,
+                                                             float* __restrict__ dbias, int cols, int row_parts) {
+  __shared__ float room[16][64];
+  const int c = blockIdx.y * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;   // column of [2][cols]
   const int64_t group = blockIdx.x;
   float s = 0.f;
-  if (c < 2 * cols)
-    for (int p = row_parts * quarter / 4; p < row_parts * (quarter + 1) / 4; ++p) s += parts[(group * row_parts + p) * 2 * cols + c];
-  room[quarter][threadIdx.x & 63] = s;
+  if (c < 2 * cols) {
+    const float* from = parts + group * row_parts * 2 * cols + c;
+#pragma unroll 4
+    for (int p = row_parts * slice / 16; p < row_parts * (slice + 1) / 16; ++p) s += from[(int64_t)p * 2 * cols];
+  }
+  room[slice][threadIdx.x & 63] = s;
   __syncthreads();
-  if (quarter != 0 || c >= 2 * cols) return;
-  s = (room[0][c & 63] + room[1][c & 63]) + (room[2][c & 63] + room[3][c & 63]);
+  if (slice != 0 || c >= 2 * cols) return;
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s += room[i][threadIdx.x];
   float* to = c < cols ? dweight : dbias;
   if (to) to[group * cols + (c < cols ? c : c - cols)] = s;
 }
@@ -322,31 +433,62 @@ constexpr int MOST_COLS = 8192;   // of a row kept in registers
 
 int status() { return hipGetLastError() == hipSuccess ? JENGA_OK : JENGA_EHIP; }
 
+template <typename X, typename P, bool E4M3, int NV, int WPR>
+void run_norm_rows(const NormArgs& a, hipStream_t st) {
+  const int64_t rows_at_once = 4 / WPR, wanted = (a.rows + rows_at_once - 1) / rows_at_once;
+  norm_kernel<X, P, E4M3, NV, WPR><<<(unsigned)std::min<int64_t>(wanted, 256 * norm_per_cu<X, P, E4M3, NV>()), 256, 0, st>>>(a);
+}
+
 template <typename X, typename P, bool E4M3>
 int run_norm(const NormArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)std::min<int64_t>((a.rows + 3) / 4, 1 << 20);
-  if (a.cols <= 512) norm_kernel<X, P, E4M3, 1><<<grid, 256, 0, st>>>(a);
-  else if (a.cols <= 2048) norm_kernel<X, P, E4M3, 4><<<grid, 256, 0, st>>>(a);
-  else if (a.cols <= 5120) norm_kernel<X, P, E4M3, 10><<<grid, 256, 0, st>>>(a);
-  else if (a.cols <= MOST_COLS) norm_kernel<X, P, E4M3, 16><<<grid, 256, 0, st>>>(a);
-  else norm_long_kernel<X, P, E4M3><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), 1024, 0, st>>>(a);
+  if (a.cols > MOST_COLS || a.cols < 8 || (E4M3 && a.cols % 8 != 0)) {
+    norm_long_kernel<X, P, E4M3><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), 1024, 0, st>>>(a);
+    return status();
+  }
+  if (a.cols <= 512) run_norm_rows<X, P, E4M3, 1, 1>(a, st);
+  else if (a.cols <= 1024) run_norm_rows<X, P, E4M3, 1, 2>(a, st);
+  else if (a.cols <= 1536) run_norm_rows<X, P, E4M3, 3, 1>(a, st);
+  else if (a.cols <= 2048) run_norm_rows<X, P, E4M3, 1, 4>(a, st);
+  else if (a.cols <= 4096) run_norm_rows<X, P, E4M3, 2, 4>(a, st);
+  else if (a.cols <= 6144) run_norm_rows<X, P, E4M3, 3, 4>(a, st);
+  else run_norm_rows<X, P, E4M3, 4, 4>(a, st);
   return status();
 }
 
+template <typename X, typename P, int NV, int WPR>
+void run_grad_rows(const NormArgs& a, unsigned groups, hipStream_t st) {
+  constexpr int WAVES = grad_waves(WPR);
+  norm_grad_kernel<X, P, NV, WPR><<<groups * (unsigned)a.row_parts, 64 * WAVES, WAVES > WPR ? (size_t)a.cols * 8 : 0, st>>>(a);
+}
+
 template <typename X, typename P>
-int run_grad(const NormArgs& a, unsigned groups, float* dweight, float* dbias, hipStream_t st) {
-  const unsigned wgs = groups * (unsigned)a.row_parts;
-  const size_t lds = (size_t)a.cols * 8;
-  if (a.cols <= 512) norm_grad_kernel<X, P, 1, 1><<<wgs, 256, lds, st>>>(a);
-  else if (a.cols <= 2048) norm_grad_kernel<X, P, 4, 1><<<wgs, 256, lds, st>>>(a);
-  else if (a.cols <= 4096) norm_grad_kernel<X, P, 2, 4><<<wgs, 256, 0, st>>>(a);
-  else if (a.cols <= MOST_COLS) norm_grad_kernel<X, P, 4, 4><<<wgs, 256, 0, st>>>(a);
-  else {
+int run_grad(NormArgs a, unsigned groups, float* dweight, float* dbias, hipStream_t st) {
+  // as many workgroups as the chip holds, eight rows each at least
+  const bool in_registers = a.cols <= MOST_COLS && a.cols >= 8;
+  const int per_cu = !in_registers ? 4 : a.cols <= 1024 ? grad_per_cu<1>() : a.cols <= 1536 ? grad_per_cu<3>() : a.cols <= 2048 ? grad_per_cu<1>() :
+                     a.cols <= 4096 ? grad_per_cu<2>() : a.cols <= 6144 ? grad_per_cu<3>() : 1;
+  const int64_t rows = std::min(a.rows, a.group_rows);
+  a.row_parts = (int)std::max<int64_t>(1, std::min<int64_t>(256 * per_cu / groups, (rows + 7) / 8));
+  if (!in_registers) {
     norm_grad_long_kernel<X, P><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), 1024, 0, st>>>(a);
-    if (a.parts) norm_grad_columns_kernel<X><<<dim3(wgs, (a.cols + 255) / 256), 256, 0, st>>>(a);
+    if (a.parts) norm_grad_columns_kernel<X><<<dim3(groups * a.row_parts, (a.cols + 255) / 256), 256, 0, st>>>(a);
+  } else if (a.cols <= 512) {
+    run_grad_rows<X, P, 1, 1>(a, groups, st);
+  } else if (a.cols <= 1024) {
+    run_grad_rows<X, P, 1, 2>(a, groups, st);
+  } else if (a.cols <= 1536) {
+    run_grad_rows<X, P, 3, 1>(a, groups, st);
+  } else if (a.cols <= 2048) {
+    run_grad_rows<X, P, 1, 4>(a, groups, st);
+  } else if (a.cols <= 4096) {
+    run_grad_rows<X, P, 2, 4>(a, groups, st);
+  } else if (a.cols <= 6144) {
+    run_grad_rows<X, P, 3, 4>(a, groups, st);
+  } else {
+    run_grad_rows<X, P, 2, 8>(a, groups, st);
   }
   if (a.parts)
-    norm_grad_sum_kernel<<<dim3(groups, (2 * a.cols + 63) / 64), 256, 0, st>>>(a.parts, dweight, dbias, a.cols, a.row_parts);
+    norm_grad_sum_kernel<<<dim3(groups, (2 * a.cols + 63) / 64), 1024, 0, st>>>(a.parts, dweight, dbias, a.cols, a.row_parts);
   return status();
 }
 
@@ -412,7 +554,6 @@ int jenga_layer_norm_grad(const jenga_norm_config* cfg, const void* x, const voi
   a.rstd = (float*)rstd;
   a.dx = dx;
   a.parts = dweight_or_null || dbias_or_null ? (float*)workspace : nullptr;
-  a.row_parts = jenga::norm_grad_parts(*cfg);
   hipStream_t st = (hipStream_t)stream;
   const bool f32_params = cfg->param_type == JENGA_F32;
 #define JENGA_NORM_GRAD(X, P) return run_grad<X, P>(a, (unsigned)groups, dweight_or_null, dbias_or_null, st)
