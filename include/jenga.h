@@ -323,7 +323,7 @@ typedef struct {
  * result's norm); for float32 results the operands are widened, and nothing is cut off.
  * The gradients are products of the same kind: of a, from out's gradient in rows of blocks and b's transpose; of b,
  * from the transposes of out's gradient (blocks of 1 x 128) and of a (128 x 128).
- * JENGA_EUNSUPPORTED: more than 2^23 tiles of 128 x 128, k above 2^17.
+ * JENGA_EUNSUPPORTED: more than 2^23 tiles of 128 x 128, k above 2^17, n above 2^22.
  */
 int jenga_matmul(const jenga_matmul_config* cfg, const void* a, const uint8_t* a_scale, const void* b,
                  const uint8_t* b_scale, const float* bias_or_null, void* out, void* stream);

@@ -196,7 +196,7 @@ int matmul_args_ok(const jenga_matmul_config* c, const void* a, const uint8_t* a
   const int64_t size = type_size(c->out_type);
   if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4) || !aligned(bias, 4) || !aligned(out, size))
     return JENGA_EINVAL;
-  if (c->k > MOST_COLS || c->m > 1ll << 30 || c->out_stride > 1ll << 31) return JENGA_EUNSUPPORTED;
+  if (c->k > MOST_COLS || c->m > 1ll << 30 || c->n > 1 << 22 || c->out_stride > 1ll << 31) return JENGA_EUNSUPPORTED;
   if ((c->m + 127) / 128 * (((int64_t)c->n + 127) / 128) > 1ll << 23) return JENGA_EUNSUPPORTED;
   if (c->m == 0) return JENGA_OK;
   const int64_t scales = ((int64_t)c->k + 511) / 512 * 4;

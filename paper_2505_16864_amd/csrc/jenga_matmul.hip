@@ -16,6 +16,7 @@ namespace {
 using namespace jenga;
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -127,6 +128,70 @@ __device__ __forceinline__ f32x16 multiply(const Fragment<true>& x, int xs, cons
   return acc;
 }
 
+// The same for 16 rows and a whole block, a row in lanes l, l + 16, l + 32 and l + 48.
+__device__ __forceinline__ f32x4 multiply16(const Fragment<false>& x, int xs, const Fragment<false>& y, int ys, f32x4 acc) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x.v, y.v, acc, 0, 0, 0, xs, 0, ys);
+#else
+  return acc;
+#endif
+}
+__device__ __forceinline__ f32x4 multiply16(const Fragment<true>& x, int xs, const Fragment<true>& y, int ys, f32x4 acc) {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.wide(i, xs & 255), y.wide(i, ys & 255), acc, 0, 0, 0);
+#endif
+  return acc;
+}
+
+__device__ __forceinline__ i32x8 bytes32(const uint8_t* p) {
+  const uint4 v[2] = {*(const uint4*)p, *(const uint4*)(p + 16)};
+  i32x8 r;
+  __builtin_memcpy(&r, v, 32);
+  return r;
+}
+
+// Up to 16 rows of a: the weight is read once and is what takes the time, so there are no tiles.  A workgroup makes 16 columns; its eight
+// wavefronts take a block of k each in turn, straight from memory into registers, four turns ahead, and add their sums up in LDS.
+// 1 x 15360 x 5120: 14.3 us, 5.5 TB/s.
+template <typename O, bool EXACT>
+__global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs g) {
+  constexpr int WAVES = 8, AHEAD = 4;
+  __shared__ float sums[WAVES][256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, piece = (lane >> 4) * 32;
+  const int col0 = blockIdx.x * 16;
+  const size_t pitch = (size_t)g.steps * 128;
+  const int64_t a_row = min((int64_t)i16, g.m - 1);   // rows and columns past the end: the last one again, and not stored
+  const uint8_t *a = g.a + a_row * pitch + piece, *a_scale = g.a_scale + a_row * g.quads * 4;
+  const uint8_t *b = g.b + (size_t)min(col0 + i16, g.n - 1) * pitch + piece, *b_scale = g.b_scale + (size_t)(col0 >> 7) * g.quads * 4;
+  f32x4 acc = 0.f;
+  for (int s0 = wave; s0 < g.steps; s0 += AHEAD * WAVES) {
+    Fragment<EXACT> fb[AHEAD], fa[AHEAD];
+    int sb[AHEAD], sa[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int s = s0 + u * WAVES;
+      if (s < g.steps) {
+        fb[u].v = bytes32(b + (size_t)s * 128);
+        sb[u] = b_scale[s];
+        fa[u].v = bytes32(a + (size_t)s * 128);
+        sa[u] = a_scale[s];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (s0 + u * WAVES < g.steps) acc = multiply16(fb[u], sb[u], fa[u], sa[u], acc);
+  }
+  *(f32x4*)&sums[wave][i16 * 16 + (lane >> 4) * 4] = acc;   // lane l holds row l % 16 of a, columns 4 (l / 16) to + 3
+  __syncthreads();
+  const int row = threadIdx.x >> 4, col = col0 + (threadIdx.x & 15);
+  if (threadIdx.x >= 256 || row >= g.m || col >= g.n) return;
+  float v = 0.f;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) v += sums[w][threadIdx.x];
+  ((O*)g.out)[row * g.out_stride + col] = (O)(g.bias ? v + g.bias[col] : v);
+}
+
 // 64 lanes x 16 (or 4) bytes from global memory straight into 1 KB (256 bytes) of LDS, complete when vmcnt says so.
 __device__ __forceinline__ uint64_t uniform(const uint8_t* p) {
   const uint64_t b = (uint64_t)p;
@@ -175,13 +240,24 @@ __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int* tm
 // rotated by an exclusive or with bits of the row, so that the rows of a fragment fall on all banks.  The rows of b are the rows of
 // the matrix instruction, taken in an order that puts eight neighbouring results of a row of out into a lane: two fragments j,
 // j + 1 hold columns 16 q + 8 (lane / 32) + 4 (j & 1) + 0..3 of 64.
-template <typename O, bool EXACT, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g) {
+//
+// SPLIT = 2, for fewer tiles than compute units: two such groups of wavefronts with LDS tiles of their own take every other block, and the
+// second one's sums are added to the first one's in LDS.
+template <typename O, bool EXACT, int BM, int BN, int WM, int WN, int SPLIT>
+__global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
   constexpr int MT = BM / WM / 32, NT = BN / WN / 32, COPIES = (BM + BN) / 32, STAGE = (BM + BN) * 128;
-  static_assert(WM * WN == 4 && BM % 64 == 0 && BN % 64 == 0 && BN / WN <= 128 && 128 % (BN / WN) == 0 && NT % 2 == 0, "");
-  __shared__ __attribute__((aligned(128))) uint8_t tiles[2 * STAGE + 2 * BM * 4];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
-  const uint32_t pitch = (uint32_t)g.steps * 128, lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)tiles;
+  static_assert((SPLIT == 1 || SPLIT == 2) && WM * WN == 4 && BM % 64 == 0 && BN % 64 == 0 && BN / WN <= 128 && 128 % (BN / WN) == 0 && NT % 2 == 0, "");
+  // the results of 32 rows of each wavefront go where the second tile is
+  constexpr int PITCH = BN / WN * sizeof(O), SECOND = STAGE > 4 * 32 * PITCH ? STAGE : 4 * 32 * PITCH;
+  constexpr int GROUP = STAGE + SECOND + 2 * BM * 4;
+  __shared__ __attribute__((aligned(128))) uint8_t all_tiles[SPLIT * GROUP];
+  const int group = SPLIT == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, wm = wave % WM, wn = wave / WM;
+  uint8_t* tiles = all_tiles + group * GROUP;
+  const uint32_t pitch = (uint32_t)g.steps * 128,
+                 lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)all_tiles + group * GROUP;
+  const int turns = (g.steps + SPLIT - 1) / SPLIT;
+  auto block_of = [&](int s) { return s * SPLIT + group; };   // of turn s
   const int n_tiles = g.tiles_m * g.tiles_n, xcd = blockIdx.x & 7;
   const int end = (int)((int64_t)n_tiles * (xcd + 1) >> 3);
   int t = (int)((int64_t)n_tiles * xcd >> 3) + (blockIdx.x >> 3);
@@ -216,12 +292,13 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g) {
   auto copy_one = [&](int s, int c) {
     const bool of_a = c * 32 < BM;
     copy_1kb(of_a ? a_rows : b_rows, of_a ? from_a : from_b,
-             s < g.steps ? (of_a ? c : c - BM / 32) * 32 * pitch + s * 128 : 0x80000000u,   // past the end: outside of the buffer
+             block_of(s) < g.steps ? (of_a ? c : c - BM / 32) * 32 * pitch + block_of(s) * 128 : 0x80000000u,   // past the end: outside
              lds0 + (s & 1) * STAGE + (c * 4 + wave) * 1024);
   };
   auto copy_scales = [&](int s) {
-    copy_256b((s & 3) == 0 && s < g.steps && wave < BM / 64, s0 + s, scale_from,
-              lds0 + 2 * STAGE + (s >> 2 & 1) * BM * 4 + wave % (BM / 64) * 256);
+    const int k = min(block_of(s), g.steps - 1);   // blocks past the end are zeros, times a scale that has to be a number: the last one's
+    copy_256b(s % (4 / SPLIT) == 0 && wave < BM / 64, s0 + (k & ~3), scale_from,
+              lds0 + STAGE + SECOND + (k >> 2 & 1) * BM * 4 + wave % (BM / 64) * 256);
   };
 
   f32x16 acc[MT][NT];
@@ -238,11 +315,11 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g) {
     __builtin_memcpy(OF_A ? &fa[H][I].v : &fb[H][J].v, v, 32);
   };
   auto read_scales = [&](int s) {
-    s = min(s, g.steps - 1);
-    const uint8_t* sa = tiles + 2 * STAGE + ((s >> 2 & 1) * BM + ra) * 4 + (s & 3);
+    const int k = min(block_of(s), g.steps - 1);
+    const uint8_t* sa = tiles + STAGE + SECOND + ((k >> 2 & 1) * BM + ra) * 4 + (k & 3);
 #pragma unroll
     for (int i = 0; i < MT; ++i) scale_a[i] = sa[128 * i];
-    scale_b = sb[s >> 2] >> (s & 3) * 8;
+    scale_b = sb[k >> 2] >> (k & 3) * 8;
   };
   using std::integral_constant;
   constexpr integral_constant<int, 0> n0;
@@ -285,12 +362,12 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g) {
   // The results go through LDS, so that a store takes whole rows of the wavefront's columns.  Room for each wavefront in the second LDS
   // tile, for ROWS of its rows at a time.  They are not kept in the caches: the operands that they would drive out cost more (33272 x
   // 15360 x 5120: 2.40 -> 2.17 ms).
-  constexpr int COLS = BN / WN, PITCH = COLS * sizeof(O), PIECES = PITCH / 16, FIT = STAGE / 4 / PITCH / 32 * 32,
+  constexpr int COLS = BN / WN, PIECES = PITCH / 16, FIT = SECOND / 4 / PITCH / 32 * 32,
                 ROWS = FIT < MT * 32 ? FIT : MT * 32, AT_ONCE = 64 / PIECES;   // rows that a store takes
   constexpr int STORES = MT * 32 / AT_ONCE;
   static_assert(ROWS >= 32 && MT * 32 % ROWS == 0 && PIECES <= 64 && COPIES + STORES <= 63, "");
   auto store_results = [&](int64_t row0, int col0, int rows, int cols) {
-    uint8_t* room = tiles + STAGE + wave * (STAGE / 4);
+    uint8_t* room = tiles + STAGE + wave * (SECOND / 4);
     const int out_col = col0 + wn * COLS, left = g.n - out_col;
     const bool inside = rows == BM && cols == BN;
     each<MT * 32 / ROWS>([&](auto part) {
@@ -358,9 +435,25 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g) {
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) acc[i][j] = 0.f;
-    for (int s = 0; s < g.steps; ++s) block(s);
+    for (int s = 0; s < turns; ++s) block(s);
     // everybody has read the last fragments, and nothing is on its way to LDS
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    if constexpr (SPLIT == 2) {   // the second group's sums over its own tiles, 4 bytes a lane next to each other
+      float* sums = (float*)(all_tiles + GROUP) + threadIdx.x % 256;
+      static_assert(MT * NT * 16 * 256 * 4 <= GROUP, "");
+      each<MT * NT * 16>([&](auto index) {
+        constexpr int N = decltype(index)::value;
+        if (group == 1) sums[N * 256] = acc[N / 16 % MT][N / 16 / MT][N % 16];
+      });
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+      if (group == 1) return;   // a workgroup makes one tile then
+      each<MT * NT * 16>([&](auto index) {
+        constexpr int N = decltype(index)::value;
+        acc[N / 16 % MT][N / 16 / MT][N % 16] += sums[N * 256];
+      });
+      store_results(row0, col0, rows, cols);
+      return;
+    }
     const int64_t row = row0;
     const int col = col0, height = rows, width = cols;
     t += gridDim.x >> 3;
@@ -378,20 +471,38 @@ __global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g) {
 
 // per_cu: workgroups that a compute unit holds, by LDS.  A workgroup makes several tiles, so that the first block of the next one is on its
 // way while the results of the last one are stored.
-template <typename O, bool EXACT, int BM, int BN, int WM, int WN>
+template <typename O, bool EXACT, int BM, int BN, int WM, int WN, int SPLIT>
 int run_tiles(MatmulArgs g, int per_cu, hipStream_t st) {
   g.tiles_m = (int)((g.m + BM - 1) / BM);
   g.tiles_n = (g.n + BN - 1) / BN;
-  const int tiles = g.tiles_m * g.tiles_n;
-  matmul_kernel<O, EXACT, BM, BN, WM, WN><<<std::min((tiles + 7) / 8 * 8, 256 * per_cu), 256, 0, st>>>(g);
+  const int tiles = (g.tiles_m * g.tiles_n + 7) / 8 * 8;
+  matmul_kernel<O, EXACT, BM, BN, WM, WN, SPLIT><<<SPLIT == 1 ? std::min(tiles, 256 * per_cu) : tiles, 256 * SPLIT, 0, st>>>(g);
+  return status();
+}
+
+template <typename O, bool EXACT>
+int run_rows(const MatmulArgs& g, hipStream_t st) {
+  matmul_rows_kernel<O, EXACT><<<(g.n + 15) / 16, 512, 0, st>>>(g);
   return status();
 }
 
 template <typename O, bool EXACT>
 int run_matmul(const MatmulArgs& g, hipStream_t st) {
+  if (g.m <= 16) return run_rows<O, EXACT>(g, st);
+  // Tiles of 256 x 256 read each row of either operand half as often as those of 128 x 128, a round of them (one a compute unit) takes 1.45 times
+  // as long as a round of the others (two a unit).  us, 256 -> 128: 1500 x 5120 x 5120 (120 tiles, one round each) 55.5 -> 40.7; 2048 (1 and
+  // 2 rounds) 58.2 -> 71.5; 3000 (1 and 2) 65.7 -> 79.1; 4096 (2 and 3) 118.1 -> 113.5; 33272 x 15360 (31 and 61) 2144 -> 2603.
+  // 64 x 128 where 128 x 128 would leave units idle, in two groups while there are fewer tiles than units.  us, 128 -> 64 -> 64 in groups:
+  // 64 x 5120 x 5120 (40 tiles of 64 x 128) 23.0 -> 19.0 -> 15.3; 256 (160) 33.6 -> 26.5 -> 21.9; 512 (320) 33.8 -> 28.7 -> 40.7; 1024 (640)
+  // 36.3 -> 40.5 -> 61.5; 2500 x 1536 x 1536 (480) 10.6 -> 10.7 -> 14.4.
+  // Up to 16 rows without tiles.  us, rows -> 64 x 128 in groups: 16 x 5120 x 5120 11.5 -> 14.9; 32 16.4 -> 15.1; 48 23.7 -> 15.2.
+  auto tiles = [&](int bm, int bn) { return (g.m + bm - 1) / bm * ((g.n + bn - 1) / bn); };
+  auto rounds = [&](int64_t n, int at_once) { return (n + at_once - 1) / at_once; };
   if constexpr (!EXACT)
-    if ((g.m + 255) / 256 * ((g.n + 255) / 256) >= 256) return run_tiles<O, EXACT, 256, 256, 2, 2>(g, 1, st);
-  return run_tiles<O, EXACT, 128, 128, 2, 2>(g, 2, st);
+    if (1.45 * rounds(tiles(256, 256), 256) <= rounds(tiles(128, 128), 512)) return run_tiles<O, EXACT, 256, 256, 2, 2, 1>(g, 1, st);
+  if (tiles(64, 128) <= 256) return run_tiles<O, EXACT, 64, 128, 2, 2, 2>(g, 1, st);
+  if (tiles(64, 128) <= 512) return run_tiles<O, EXACT, 64, 128, 2, 2, 1>(g, 2, st);
+  return run_tiles<O, EXACT, 128, 128, 2, 2, 1>(g, 2, st);
 }
 
 template <typename X>
