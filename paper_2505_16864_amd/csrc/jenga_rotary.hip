@@ -31,7 +31,7 @@ struct RotaryArgs {
   int count;
   Turns turns;
   const int32_t *src_of_pos, *cells;
-  int64_t tokens, units;   // units: batch * tokens
+  uint32_t tokens, units;   // units: batch * tokens, times the pairs of a head below 2^32
   int head_dim;
   int heads_per_wg;
 };
@@ -67,11 +67,11 @@ __device__ __forceinline__ bool turn_of(const Turns& t, const Pair& p, const int
   return turned;
 }
 
-// The cell of token n of batch entry b on each axis, -1: not turned.
-__device__ __forceinline__ void cells_of(const RotaryArgs& a, int64_t b, int64_t n, int cell[3]) {
+// The cell of token n, unit `unit`, on each axis, -1: not turned.
+__device__ __forceinline__ void cells_of(const RotaryArgs& a, uint32_t unit, int64_t n, int cell[3]) {
   cell[0] = cell[1] = cell[2] = -1;
   if (a.cells) {
-    const int32_t* c = a.cells + (b * a.tokens + n) * 3;
+    const int32_t* c = a.cells + (size_t)unit * 3;
     cell[0] = min(c[0], a.turns.grid.T - 1);
     cell[1] = min(c[1], a.turns.grid.H - 1);
     cell[2] = min(c[2], a.turns.grid.W - 1);
@@ -85,12 +85,12 @@ __device__ __forceinline__ void cells_of(const RotaryArgs& a, int64_t b, int64_t
 template <typename X>
 __global__ __launch_bounds__(256) void rotary_neighbours_kernel(RotaryArgs a) {
   const int pieces = a.head_dim / 8;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, unit = id / pieces;
+  const uint32_t id = blockIdx.x * 256u + threadIdx.x, unit = id / (uint32_t)pieces;
   if (unit >= a.units) return;
-  const int c = (int)(id - unit * pieces) * 8;
-  const int64_t b = unit / a.tokens, n = unit - b * a.tokens;
+  const int c = (int)(id - unit * (uint32_t)pieces) * 8;
+  const int64_t b = unit / a.tokens, n = unit % a.tokens;
   int cell[3];
-  cells_of(a, b, n, cell);
+  cells_of(a, unit, n, cell);
   float2 turn[4];
   bool turned[4], any = false;
 #pragma unroll
@@ -135,11 +135,11 @@ __global__ __launch_bounds__(256) void rotary_halves_kernel(RotaryArgs a) {
   __shared__ __attribute__((aligned(16))) X room[4][4][64 * 8];   // wavefront, head
   const int pieces = a.head_dim / 8, per_wave = 64 / pieces, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = lane / pieces, c = (lane - row * pieces) * 8;
-  const int64_t unit = ((int64_t)blockIdx.x * 4 + wave) * per_wave + row;
+  const uint32_t unit = (blockIdx.x * 4u + wave) * per_wave + row;
   if (row >= per_wave || unit >= a.units) return;
-  const int64_t b = unit / a.tokens, n = unit - b * a.tokens;
+  const int64_t b = unit / a.tokens, n = unit % a.tokens;
   int cell[3];
-  cells_of(a, b, n, cell);
+  cells_of(a, unit, n, cell);
   float2 turn[8];
   int other[8];
   bool turned[8], any = false;
@@ -187,10 +187,10 @@ __global__ __launch_bounds__(256) void rotary_halves_kernel(RotaryArgs a) {
 template <typename X, bool HALVES>
 __global__ __launch_bounds__(256) void rotary_pairs_kernel(RotaryArgs a) {
   const int half = a.head_dim / 2;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, unit = id / half;
+  const uint32_t id = blockIdx.x * 256u + threadIdx.x, unit = id / (uint32_t)half;
   if (unit >= a.units) return;
-  const int p = (int)(id - unit * half);
-  const int64_t b = unit / a.tokens, n = unit - b * a.tokens;
+  const int p = (int)(id - unit * (uint32_t)half);
+  const int64_t b = unit / a.tokens, n = unit % a.tokens;
   int c0 = 2 * p, c1 = 2 * p + 1;
   if (HALVES) {   // pair p of the axis it falls on; behind the axes neighbours
     const int e0 = a.turns.pairs[0], e1 = e0 + a.turns.pairs[1], e2 = e1 + a.turns.pairs[2];
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256) void rotary_pairs_kernel(RotaryArgs a) {
   }
   int cell[3], other;
   bool second;
-  cells_of(a, b, n, cell);
+  cells_of(a, unit, n, cell);
   float2 t;
   const bool turned = turn_of(a.turns, pair_of<HALVES>(a.turns, c0, &other, &second), cell, &t);
   const int h0 = blockIdx.y * a.heads_per_wg;
@@ -225,14 +225,14 @@ int run_rotary(const RotaryArgs& a, bool halves, hipStream_t st) {
   const int most = a.count > 1 ? std::max(a.heads[0], a.heads[1]) : a.heads[0], groups = (most + a.heads_per_wg - 1) / a.heads_per_wg;
   const int pieces = a.head_dim / 8;
   if (a.head_dim % 8 != 0 || (halves && pieces > 64)) {
-    const dim3 grid((unsigned)((a.units * (a.head_dim / 2) + 255) / 256), groups);
+    const dim3 grid((unsigned)(((int64_t)a.units * (a.head_dim / 2) + 255) / 256), groups);
     if (halves) rotary_pairs_kernel<X, true><<<grid, 256, 0, st>>>(a);
     else rotary_pairs_kernel<X, false><<<grid, 256, 0, st>>>(a);
   } else if (halves) {
     const int64_t per_wg = 64 / pieces * 4;
     rotary_halves_kernel<X><<<dim3((unsigned)((a.units + per_wg - 1) / per_wg), groups), 256, 0, st>>>(a);
   } else {
-    rotary_neighbours_kernel<X><<<dim3((unsigned)((a.units * pieces + 255) / 256), groups), 256, 0, st>>>(a);
+    rotary_neighbours_kernel<X><<<dim3((unsigned)(((int64_t)a.units * pieces + 255) / 256), groups), 256, 0, st>>>(a);
   }
   return status();
 }
@@ -403,8 +403,8 @@ extern "C" int jenga_rotary(const jenga_rotary_config* cfg, const jenga_plan* pl
   a.turns = turns_of(*cfg, table);
   a.cells = cells_or_null;
   a.src_of_pos = plan_or_null ? plan_or_null->d_src_of_pos : nullptr;
-  a.tokens = tokens;
-  a.units = batch * tokens;
+  a.tokens = (uint32_t)tokens;
+  a.units = (uint32_t)(batch * tokens);
   a.head_dim = cfg->head_dim;
   a.heads_per_wg = 8;
   const bool halves = (cfg->flags & JENGA_ROTARY_HALVES) != 0;
