@@ -287,7 +287,7 @@ typedef enum { JENGA_BF16 = 0, JENGA_F16 = 1, JENGA_F32 = 2, JENGA_E4M3 = 3 } je
  * 8-bit tensors.  A matrix of r rows and c columns is held as
  *   values  e4m3 [r][C], C = c rounded up to a multiple of 128; the columns that fill up are 0.  16-byte aligned
  *   scales  uint8 [r][S] (a block is 1 row x 128 columns) or [ceil(r / 128)][S] (128 x 128), S = ceil(c / 512) * 4;
- *           byte e + 127 for the scale 2^e of a block; the bytes that fill up a row are 0.  4-byte aligned
+ *           byte e + 127, 0 to 254, for the scale 2^e of a block; the bytes that fill up a row are 0.  4-byte aligned
  * and stands for values * 2^e.  e is the least whole number >= -127 with |x| <= 448 * 2^e for all finite x of the
  * block (0 where they are all 0): nothing saturates, and the only rounding is the one to e4m3, to nearest even.
  * What is not finite becomes NaN.
@@ -320,7 +320,8 @@ typedef struct {
  *   bias_or_null : float32 [n]
  * Sums are float32 and rounded once.  For 16-bit results the f8 matrix core multiplies, which adds eight products
  * at a time and cuts them off at 2^-13 of the largest of the eight (for normally distributed values 1.5e-5 of the
- * result's norm); for float32 results the operands are widened, and nothing is cut off.
+ * result's norm); for float32 results the operands are widened to bf16, and nothing is cut off but values * 2^e below
+ * 2^-126, which may lose digits or be taken as 0.
  * The gradients are products of the same kind: of a, from out's gradient in rows of blocks and b's transpose; of b,
  * from the transposes of out's gradient (blocks of 1 x 128) and of a (128 x 128).
  * JENGA_EUNSUPPORTED: more than 2^23 tiles of 128 x 128, k above 2^17, n above 2^22.
@@ -364,7 +365,8 @@ int jenga_layer_norm(const jenga_norm_config* cfg, const void* x, const void* we
  *   dx              : x_type, x_stride elements between rows
  *   dweight, dbias  : float32 [groups][cols] next to each other, fully overwritten, or NULL
  *   workspace       : jenga_layer_norm_grad_workspace bytes, 256-byte aligned, contents undefined after; NULL if
- *                     both of them are
+ *                     both of them are.  Calls that may run at the same time (on two streams, in graphs that are
+ *                     replayed on two streams) need one each
  * Sums are float32 and in an order that depends on the sizes alone: the same call gives the same bits.
  * JENGA_EUNSUPPORTED: more than 2^20 groups.
  */
@@ -398,7 +400,7 @@ typedef struct {
 /*
  * cos and sin of every pair and cell, axis by axis: float32 [T][dim[0]/2][2], [H][dim[1]/2][2], [W][dim[2]/2][2] one
  * behind the other, T dim[0] + H dim[1] + W dim[2] floats in HOST memory, from float64 angles.  The caller copies them
- * to the device once per grid.  Host only.
+ * to the device once per grid.  Host only.  JENGA_EINVAL, with the table undefined: an angle that is not finite.
  */
 int jenga_rotary_table(const jenga_rotary_config* cfg, float* table);
 
@@ -421,7 +423,7 @@ typedef struct {
  *                         same T, H and W, and tokens = N_pad
  *   cells               : int32 [batch][tokens][3], the cell on each axis: sequences of several grids, padded batches.
  *                         Channels of an axis where it is negative are copied; cells past the end are taken as the last
- * JENGA_EUNSUPPORTED: more than 2^24 * 256 pairs a head and tensor.
+ * JENGA_EUNSUPPORTED: more than 2^32 - 256 pairs in one head of all tokens.
  */
 int jenga_rotary(const jenga_rotary_config* cfg, const jenga_plan* plan_or_null, const int32_t* cells_or_null,
                  const float* table, const jenga_rotary_tensor* tensors, int32_t count, int64_t batch, int64_t tokens,

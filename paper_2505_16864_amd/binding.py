@@ -314,6 +314,8 @@ def jenga_quantize(x, q, scale, block_rows=1, stream=None):
 def jenga_matmul(a, a_scale, b, b_scale, out, bias=None, stream=None):
     """out [m, n] = a b^T + bias for 8-bit tensors a [m, k] (blocks of 1 x 128) and b [n, k] (128 x 128); bias float32 [n]."""
     what = "jenga_matmul"
+    if len(a.shape) != 2 or len(b.shape) != 2:
+        _refuse(what, "shapes %s, %s" % (tuple(a.shape), tuple(b.shape)))
     (m, k), n, kind = a.shape, b.shape[0], _type(out, what)
     stride = _matrix(out, what, m, n)
     scales = scale_columns(k)
@@ -385,7 +387,7 @@ def jenga_layer_norm_grad(x, dy, dx, weight, mean, rstd, dweight=None, dbias=Non
     what = "jenga_layer_norm_grad"
     cfg = _norm_config(what, x, dy, weight, None, group_rows, weight_offset, 0.0)
     rows, cols = x.shape
-    if cfg.y_type != cfg.x_type or dx.dtype != x.dtype or _matrix(dx, what, rows, cols) != cfg.x_stride:
+    if cfg.y_type != cfg.x_type or dx.dtype != x.dtype or _matrix(dx, what, rows, cols) != cfg.x_stride and rows > 1:
         _refuse(what, "dy is not of x's type, or dx is not laid out as x is")
     if mean is None or rstd is None:
         _refuse(what, "mean and rstd of the forward pass are wanted")
@@ -440,6 +442,8 @@ def jenga_rotary(cfg, table, q, q_out, k=None, k_out=None, cells=None, plan=None
     plan: tokens in its curve order (a curve-side tensor transposed to this shape); cells: int32 [batch, tokens, 3]."""
     what = "jenga_rotary"
     kind = _type(q, what)
+    if (k is None) != (k_out is None):
+        _refuse(what, "k without k_out, or the other way round")
     if k is None:
         tensors = (jenga_rotary_tensor * 1)(_rotary_tensor(cfg, q, q_out, what))
     else:
@@ -463,6 +467,8 @@ def jenga_forward_rotary(plan, cfg, table, q_thw, k_thw, v_thw, q_curve, k_curve
                          stream=None):
     """q_thw, k_thw, v_thw: [batch, N_v + N_c, heads, head_dim], tokens the same distance apart in all three."""
     what = "jenga_forward_rotary"
+    if len(q_thw.shape) != 4:
+        _refuse(what, "shape %s" % (tuple(q_thw.shape),))
     batch, tokens, heads, dim = q_thw.shape
     stride = q_thw.stride(1) if tokens > 1 else q_thw.stride(0) if batch > 1 else heads * dim
     for t in (q_thw, k_thw, v_thw):

@@ -331,6 +331,7 @@ int jenga_rotary_table(const jenga_rotary_config* c, float* table) {
     for (int n = 0; n < cells[a]; ++n)
       for (int i = 0; i < c->dim[a] / 2; ++i) {
         const double angle = (c->origin[a] + c->step[a] * n) * std::pow(c->theta, -2.0 * i / c->dim[a]);
+        if (!std::isfinite(angle)) return JENGA_EINVAL;
         *table++ = (float)std::cos(angle);
         *table++ = (float)std::sin(angle);
       }

@@ -72,6 +72,8 @@ class CarveLayer:
         """Whole path on thw-side bf16 tensors [batch, N_v+N_c, heads, d]; returns the thw-side output.  With rotary positions they may
         be columns of one projection."""
         if self.rotary is not None:
+            if q.shape != self.out_thw.shape:   # the plan's sizes are not the call's to see
+                raise ValueError("q, k and v of shape %s, not %s" % (tuple(q.shape), tuple(self.out_thw.shape)))
             B.jenga_forward_rotary(self.plan, self.rotary, self.rotary_table, q, k, v, self.q_c, self.k_c, self.v_c, self.sel_count,
                                    self.sel_index, self.mask, self.ws_select, self.ws_select.numel(), self.o_c, self.lse, self.ws_attn,
                                    self.ws_attn.numel(), self.out_thw, self._stream())

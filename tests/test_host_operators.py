@@ -221,3 +221,23 @@ def test_the_binding_refuses():
     refused(J.jenga_rotary, cfg, table, h, h.float())
     refused(J.jenga_rotary, cfg, table, h[..., :4], h[..., :4])
     refused(J.jenga_rotary, cfg, table, h, h, cells=torch.zeros(4, 3, dtype=torch.int32))
+
+
+def test_the_binding_refuses_missing_and_flat_tensors():
+    cfg, table = J.make_rotary(1, 2, 2, 8, (2, 2, 4)), torch.zeros(2 + 4 + 8)
+    h, q, s = torch.zeros(1, 4, 2, 8, dtype=torch.bfloat16), torch.zeros(4, 128, dtype=torch.uint8), torch.zeros(4, 4, dtype=torch.uint8)
+    for call in (lambda: J.jenga_rotary(cfg, table, h, h, k=h), lambda: J.jenga_rotary(cfg, table, h, h, k_out=h),
+                 lambda: J.jenga_matmul(q.view(2, 2, 128), s, q, s[:1], torch.zeros(4, 4)),
+                 lambda: J.jenga_matmul(q, s, q.view(-1), s[:1], torch.zeros(4, 4)),
+                 lambda: J.jenga_forward_rotary(None, cfg, table, h[0], h[0], h[0], *[None] * 13)):
+        with pytest.raises(J.JengaError) as e:
+            call()
+        assert e.value.status == EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(step=(1e308, 1.0, 1.0)), dict(theta=1e-300, origin=(0.0, 0.0, 1e150))])
+def test_rotary_table_refuses_angles_that_are_not_finite(bad):
+    cfg = J.make_rotary(3, 4, 5, 16, (4, 2, 6), **bad)
+    with pytest.raises(J.JengaError) as e:
+        J.jenga_rotary_table(cfg, np.zeros(3 * 4 + 4 * 2 + 5 * 6, dtype=np.float32))
+    assert e.value.status == EINVAL
