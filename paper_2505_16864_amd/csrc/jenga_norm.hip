@@ -186,32 +186,32 @@ __global__ __launch_bounds__(256, (norm_per_cu<X, P, E4M3, NV>())) void norm_ker
   }
 }
 
-// Sum over the 1024 threads of a workgroup; all of them get it.
+// Sum over the threads of a workgroup, up to 1024; all of them get it.
 __device__ __forceinline__ float block_sum(float v, float* room) {
   v = wave_sum_f32(v);
   __syncthreads();   // the room is free
   if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
   __syncthreads();
   float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) s += room[i];
+  for (int i = 0; i < (int)blockDim.x / 64; ++i) s += room[i];
   return s;
 }
 
-// Rows too long for a wavefront's registers: a workgroup each, read again for each of the three passes.
+// Rows too long for registers, and those that norm_kernel's pieces do not fit: a workgroup each, read again for each of the three
+// passes.
 template <typename X, typename P, bool E4M3>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
   __shared__ float room[16];
-  const int whole = (a.cols + 8191) & ~8191;   // every thread takes every turn: the scales of a block are 16 lanes' work
+  const int step = blockDim.x * 8, whole = (a.cols + step - 1) / step * step;   // every thread takes every turn: a block's scale is 16 lanes' work
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const X* x = (const X*)a.x + row * a.x_stride;
     float sum = 0.f, square = 0.f;
-    for (int col = threadIdx.x * 8; col < a.cols; col += 8192) {
+    for (int col = threadIdx.x * 8; col < a.cols; col += step) {
       const f32x8 f = Eight<X>::wide(load_eight(x + col, a.cols - col));
       sum += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
     }
     const float mean = block_sum(sum, room) / (float)a.cols;
-    for (int col = threadIdx.x * 8; col < a.cols; col += 8192) {
+    for (int col = threadIdx.x * 8; col < a.cols; col += step) {
       const f32x8 f = Eight<X>::wide(load_eight(x + col, a.cols - col));
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
       if (a.rstd) a.rstd[row] = rstd;
     }
     const int64_t group = row / a.group_rows;
-    for (int col = threadIdx.x * 8; col < whole; col += 8192) {
+    for (int col = threadIdx.x * 8; col < whole; col += step) {
       f32x8 w = 0.f, b = 0.f, y = 0.f;
       if (col < a.cols) {
         const f32x8 f = Eight<X>::wide(load_eight(x + col, a.cols - col));
@@ -357,17 +357,18 @@ __global__ __launch_bounds__(64 * grad_waves(WPR), (grad_per_cu<NV>())) void nor
   }
 }
 
-// Rows too long for that: dx by a workgroup per row, the sums of the columns by a thread per column.
+// Rows too long for that, or of less than eight columns: dx by a workgroup per row, the sums of the columns by a thread per column.
 template <typename X, typename P>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormArgs a) {
   __shared__ float room[16];
+  const int step = blockDim.x * 8;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const X *x = (const X*)a.x + row * a.x_stride, *dy = (const X*)a.dy + row * a.y_stride;
     const P* weight = (const P*)a.weight + row / a.group_rows * a.param_stride;
     const float mean = a.mean[row], rstd = a.rstd[row];
     float sum_g = 0.f, sum_gh = 0.f;
     for (int pass = 0; pass < 2; ++pass) {
-      for (int col = threadIdx.x * 8; col < a.cols; col += 8192) {
+      for (int col = threadIdx.x * 8; col < a.cols; col += step) {
         const int n = a.cols - col;
         f32x8 w = a.w0, d;
         if (a.weight) w += Eight<P>::wide(load_eight(weight + col, n));
@@ -405,24 +406,26 @@ __global__ __launch_bounds__(256) void norm_grad_columns_kernel(NormArgs a) {
   to[a.cols + col] = db;
 }
 
-// Adds up the parts of each group: 64 columns a workgroup, sixteen wavefronts a sixteenth of the parts each, in order.
+// Adds up the parts of each group: WIDE columns a workgroup, the parts in slices of consecutive ones that follow each other.
+template <int WIDE>
 __global__ __launch_bounds__(1024) void norm_grad_sum_kernel(const float* __restrict__ parts, float* __restrict__ dweight,
                                                              float* __restrict__ dbias, int cols, int row_parts) {
-  __shared__ float room[16][64];
-  const int c = blockIdx.y * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;   // column of [2][cols]
+  constexpr int SLICES = 1024 / WIDE;
+  __shared__ float room[SLICES][WIDE];
+  const int x = threadIdx.x % WIDE, c = blockIdx.y * WIDE + x, slice = threadIdx.x / WIDE;   // column of [2][cols]
   const int64_t group = blockIdx.x;
   float s = 0.f;
   if (c < 2 * cols) {
     const float* from = parts + group * row_parts * 2 * cols + c;
 #pragma unroll 4
-    for (int p = row_parts * slice / 16; p < row_parts * (slice + 1) / 16; ++p) s += from[(int64_t)p * 2 * cols];
+    for (int p = row_parts * slice / SLICES; p < row_parts * (slice + 1) / SLICES; ++p) s += from[(int64_t)p * 2 * cols];
   }
-  room[slice][threadIdx.x & 63] = s;
+  room[slice][x] = s;
   __syncthreads();
   if (slice != 0 || c >= 2 * cols) return;
   s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s += room[i][threadIdx.x];
+  for (int i = 0; i < SLICES; ++i) s += room[i][x];
   float* to = c < cols ? dweight : dbias;
   if (to) to[group * cols + (c < cols ? c : c - cols)] = s;
 }
@@ -433,6 +436,10 @@ constexpr int MOST_COLS = 8192;   // of a row kept in registers
 
 int status() { return hipGetLastError() == hipSuccess ? JENGA_OK : JENGA_EHIP; }
 
+// Eight columns a thread, whole wavefronts, 1024 threads at most.  (1024 for short rows too: 12068 x 777 float32
+// to 8 bits 143 us instead of 25, 60000 x 5 690 instead of 64.)
+int long_threads(int cols) { return std::min((cols + 511) / 512 * 64, 1024); }
+
 template <typename X, typename P, bool E4M3, int NV, int WPR>
 void run_norm_rows(const NormArgs& a, hipStream_t st) {
   const int64_t rows_at_once = 4 / WPR, wanted = (a.rows + rows_at_once - 1) / rows_at_once;
@@ -442,7 +449,7 @@ void run_norm_rows(const NormArgs& a, hipStream_t st) {
 template <typename X, typename P, bool E4M3>
 int run_norm(const NormArgs& a, hipStream_t st) {
   if (a.cols > MOST_COLS || a.cols < 8 || (E4M3 && a.cols % 8 != 0)) {
-    norm_long_kernel<X, P, E4M3><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), 1024, 0, st>>>(a);
+    norm_long_kernel<X, P, E4M3><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), long_threads(a.cols), 0, st>>>(a);
     return status();
   }
   if (a.cols <= 512) run_norm_rows<X, P, E4M3, 1, 1>(a, st);
@@ -470,7 +477,7 @@ int run_grad(NormArgs a, unsigned groups, float* dweight, float* dbias, hipStrea
   const int64_t rows = std::min(a.rows, a.group_rows);
   a.row_parts = (int)std::max<int64_t>(1, std::min<int64_t>(256 * per_cu / groups, (rows + 7) / 8));
   if (!in_registers) {
-    norm_grad_long_kernel<X, P><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), 1024, 0, st>>>(a);
+    norm_grad_long_kernel<X, P><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), long_threads(a.cols), 0, st>>>(a);
     if (a.parts) norm_grad_columns_kernel<X><<<dim3(groups * a.row_parts, (a.cols + 255) / 256), 256, 0, st>>>(a);
   } else if (a.cols <= 512) {
     run_grad_rows<X, P, 1, 1>(a, groups, st);
@@ -487,8 +494,12 @@ int run_grad(NormArgs a, unsigned groups, float* dweight, float* dbias, hipStrea
   } else {
     run_grad_rows<X, P, 2, 8>(a, groups, st);
   }
-  if (a.parts)
-    norm_grad_sum_kernel<<<dim3(groups, (2 * a.cols + 63) / 64), 1024, 0, st>>>(a.parts, dweight, dbias, a.cols, a.row_parts);
+  if (!a.parts) return status();
+  // 64 columns a workgroup, 32 while that leaves compute units idle.  Gradient in us, 64 -> 32: 12068 x 777 (25 workgroups of 64) 31.7 ->
+  // 29.5; 2000 x 1536 (48) 20.2 -> 19.9; 600 x 8192 in 5 groups (1280) 28.7 -> 31.8.
+  const unsigned wide = (2 * a.cols + 63) / 64;
+  if (groups * wide < 256) norm_grad_sum_kernel<32><<<dim3(groups, 2 * wide), 1024, 0, st>>>(a.parts, dweight, dbias, a.cols, a.row_parts);
+  else norm_grad_sum_kernel<64><<<dim3(groups, wide), 1024, 0, st>>>(a.parts, dweight, dbias, a.cols, a.row_parts);
   return status();
 }
 

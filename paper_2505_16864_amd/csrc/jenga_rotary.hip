@@ -220,20 +220,22 @@ __global__ __launch_bounds__(256) void rotary_pairs_kernel(RotaryArgs a) {
 
 int status() { return hipGetLastError() == hipSuccess ? JENGA_OK : JENGA_EHIP; }
 
+// A workgroup takes eight heads of its tokens, so that a token's angles are looked up for eight, but four while that makes fewer than four
+// workgroups a compute unit.  us, 8 -> 4: 2 x 6034 tokens x 8 heads x 64 (378 workgroups) 13.2 -> 12.5, halves 17.0 -> 14.1, float32
+// halves 24.8 -> 22.2; 31712 x 12 x 128 (3964) 80.8 -> 83.5, halves 84.6 -> 85.7.
 template <typename X>
-int run_rotary(const RotaryArgs& a, bool halves, hipStream_t st) {
-  const int most = a.count > 1 ? std::max(a.heads[0], a.heads[1]) : a.heads[0], groups = (most + a.heads_per_wg - 1) / a.heads_per_wg;
-  const int pieces = a.head_dim / 8;
-  if (a.head_dim % 8 != 0 || (halves && pieces > 64)) {
-    const dim3 grid((unsigned)(((int64_t)a.units * (a.head_dim / 2) + 255) / 256), groups);
-    if (halves) rotary_pairs_kernel<X, true><<<grid, 256, 0, st>>>(a);
-    else rotary_pairs_kernel<X, false><<<grid, 256, 0, st>>>(a);
-  } else if (halves) {
-    const int64_t per_wg = 64 / pieces * 4;
-    rotary_halves_kernel<X><<<dim3((unsigned)((a.units + per_wg - 1) / per_wg), groups), 256, 0, st>>>(a);
-  } else {
-    rotary_neighbours_kernel<X><<<dim3((unsigned)(((int64_t)a.units * pieces + 255) / 256), groups), 256, 0, st>>>(a);
-  }
+int run_rotary(RotaryArgs a, bool halves, hipStream_t st) {
+  const int most = a.count > 1 ? std::max(a.heads[0], a.heads[1]) : a.heads[0], pieces = a.head_dim / 8;
+  const bool by_pairs = a.head_dim % 8 != 0 || (halves && pieces > 64);
+  const int64_t per_wg = by_pairs || !halves ? 256 : 64 / pieces * 4;   // threads, or tokens
+  const int64_t work = by_pairs ? (int64_t)a.units * (a.head_dim / 2) : halves ? a.units : (int64_t)a.units * pieces;
+  const int64_t wgs = (work + per_wg - 1) / per_wg;
+  a.heads_per_wg = wgs * ((most + 7) / 8) < 1024 ? 4 : 8;
+  const dim3 grid((unsigned)wgs, (most + a.heads_per_wg - 1) / a.heads_per_wg);
+  if (by_pairs && halves) rotary_pairs_kernel<X, true><<<grid, 256, 0, st>>>(a);
+  else if (by_pairs) rotary_pairs_kernel<X, false><<<grid, 256, 0, st>>>(a);
+  else if (halves) rotary_halves_kernel<X><<<grid, 256, 0, st>>>(a);
+  else rotary_neighbours_kernel<X><<<grid, 256, 0, st>>>(a);
   return status();
 }
 
@@ -406,7 +408,6 @@ extern "C" int jenga_rotary(const jenga_rotary_config* cfg, const jenga_plan* pl
   a.tokens = (uint32_t)tokens;
   a.units = (uint32_t)(batch * tokens);
   a.head_dim = cfg->head_dim;
-  a.heads_per_wg = 8;
   const bool halves = (cfg->flags & JENGA_ROTARY_HALVES) != 0;
   hipStream_t st = (hipStream_t)stream;
   if (cfg->type == JENGA_BF16) return run_rotary<__bf16>(a, halves, st);
