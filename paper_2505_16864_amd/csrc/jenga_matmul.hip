@@ -151,45 +151,60 @@ __device__ __forceinline__ i32x8 bytes32(const uint8_t* p) {
   return r;
 }
 
-// Up to 16 rows of a: the weight is read once and is what takes the time, so there are no tiles.  A workgroup makes 16 columns; its eight
+// Up to 16 R rows of a: the weight is read once and is what takes the time, so there are no tiles.  A workgroup makes 16 columns; its eight
 // wavefronts take a block of k each in turn, straight from memory into registers, four turns ahead, and add their sums up in LDS.
 // 1 x 15360 x 5120: 14.3 us, 5.5 TB/s.
-template <typename O, bool EXACT>
+template <typename O, bool EXACT, int R>
 __global__ __launch_bounds__(512) void matmul_rows_kernel(MatmulArgs g) {
   constexpr int WAVES = 8, AHEAD = 4;
-  __shared__ float sums[WAVES][256];
+  __shared__ float sums[WAVES][R * 256];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i16 = lane & 15, piece = (lane >> 4) * 32;
   const int col0 = blockIdx.x * 16;
   const size_t pitch = (size_t)g.steps * 128;
-  const int64_t a_row = min((int64_t)i16, g.m - 1);   // rows and columns past the end: the last one again, and not stored
-  const uint8_t *a = g.a + a_row * pitch + piece, *a_scale = g.a_scale + a_row * g.quads * 4;
+  // rows and columns past the end: the last one again, and not stored
+  const uint8_t *a[R], *a_scale[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t row = min((int64_t)(16 * r + i16), g.m - 1);
+    a[r] = g.a + row * pitch + piece;
+    a_scale[r] = g.a_scale + row * g.quads * 4;
+  }
   const uint8_t *b = g.b + (size_t)min(col0 + i16, g.n - 1) * pitch + piece, *b_scale = g.b_scale + (size_t)(col0 >> 7) * g.quads * 4;
-  f32x4 acc = 0.f;
+  f32x4 acc[R] = {};
   for (int s0 = wave; s0 < g.steps; s0 += AHEAD * WAVES) {
-    Fragment<EXACT> fb[AHEAD], fa[AHEAD];
-    int sb[AHEAD], sa[AHEAD];
+    Fragment<EXACT> fb[AHEAD], fa[AHEAD][R];
+    int sb[AHEAD], sa[AHEAD][R];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int s = s0 + u * WAVES;
       if (s < g.steps) {
         fb[u].v = bytes32(b + (size_t)s * 128);
         sb[u] = b_scale[s];
-        fa[u].v = bytes32(a + (size_t)s * 128);
-        sa[u] = a_scale[s];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          fa[u][r].v = bytes32(a[r] + (size_t)s * 128);
+          sa[u][r] = a_scale[r][s];
+        }
       }
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
-      if (s0 + u * WAVES < g.steps) acc = multiply16(fb[u], sb[u], fa[u], sa[u], acc);
-  }
-  *(f32x4*)&sums[wave][i16 * 16 + (lane >> 4) * 4] = acc;   // lane l holds row l % 16 of a, columns 4 (l / 16) to + 3
-  __syncthreads();
-  const int row = threadIdx.x >> 4, col = col0 + (threadIdx.x & 15);
-  if (threadIdx.x >= 256 || row >= g.m || col >= g.n) return;
-  float v = 0.f;
+      if (s0 + u * WAVES < g.steps)
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) v += sums[w][threadIdx.x];
-  ((O*)g.out)[row * g.out_stride + col] = (O)(g.bias ? v + g.bias[col] : v);
+        for (int r = 0; r < R; ++r) acc[r] = multiply16(fb[u], sb[u], fa[u][r], sa[u][r], acc[r]);
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)   // lane l holds row l % 16 of a, columns 4 (l / 16) to + 3
+    *(f32x4*)&sums[wave][(16 * r + i16) * 16 + (lane >> 4) * 4] = acc[r];
+  __syncthreads();
+  for (int i = threadIdx.x; i < R * 256; i += 512) {
+    const int row = i >> 4, col = col0 + (i & 15);
+    if (row >= g.m || col >= g.n) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v += sums[w][i];
+    ((O*)g.out)[row * g.out_stride + col] = (O)(g.bias ? v + g.bias[col] : v);
+  }
 }
 
 // 64 lanes x 16 (or 4) bytes from global memory straight into 1 KB (256 bytes) of LDS, complete when vmcnt says so.
@@ -231,33 +246,26 @@ __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int* tm
   *tm = stripe * 8 + in - *tn * high;
 }
 
-// Four wavefronts, WM x WN, make BM x BN results, one tile after the other.  Blocks of 128 columns (bytes) of either operand are copied
-// into one of two LDS tiles while the other is multiplied; within a block the products of one half of the columns run while the
+// Four wavefronts, 2 x 2, make BM x BN results, one tile after the other.  Blocks of 128 columns (bytes) of either operand are copied
+// into one of STAGES LDS tiles while another is multiplied; within a block the products of one half of the columns run while the
 // fragments of the next half are read into registers.  So the reads of an LDS tile end in the middle of its block, and that is where
-// the barrier is: behind it the next tile is complete, and the one after it goes over this one.
+// the barrier is: behind it the next tile is complete, and the one STAGES blocks on goes over this one.
 //
 // A copy instruction takes 8 whole rows of 128 bytes: first their left halves, then the right ones.  The 16-byte pieces of a half row are
 // rotated by an exclusive or with bits of the row, so that the rows of a fragment fall on all banks.  The rows of b are the rows of
 // the matrix instruction, taken in an order that puts eight neighbouring results of a row of out into a lane: two fragments j,
 // j + 1 hold columns 16 q + 8 (lane / 32) + 4 (j & 1) + 0..3 of 64.
-//
-// SPLIT = 2, for fewer tiles than compute units: two such groups of wavefronts with LDS tiles of their own take every other block, and the
-// second one's sums are added to the first one's in LDS.
-template <typename O, bool EXACT, int BM, int BN, int WM, int WN, int SPLIT>
-__global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
-  constexpr int MT = BM / WM / 32, NT = BN / WN / 32, COPIES = (BM + BN) / 32, STAGE = (BM + BN) * 128;
-  static_assert((SPLIT == 1 || SPLIT == 2) && WM * WN == 4 && BM % 64 == 0 && BN % 64 == 0 && BN / WN <= 128 && 128 % (BN / WN) == 0 && NT % 2 == 0, "");
-  // the results of 32 rows of each wavefront go where the second tile is
-  constexpr int PITCH = BN / WN * sizeof(O), SECOND = STAGE > 4 * 32 * PITCH ? STAGE : 4 * 32 * PITCH;
-  constexpr int GROUP = STAGE + SECOND + 2 * BM * 4;
-  __shared__ __attribute__((aligned(128))) uint8_t all_tiles[SPLIT * GROUP];
-  const int group = SPLIT == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, wm = wave % WM, wn = wave / WM;
-  uint8_t* tiles = all_tiles + group * GROUP;
+template <typename O, bool EXACT, int BM, int BN, int STAGES>
+__global__ __launch_bounds__(256) void matmul_kernel(MatmulArgs g) {
+  constexpr int WM = 2, WN = 2, MT = BM / WM / 32, NT = BN / WN / 32, COPIES = (BM + BN) / 32, STAGE = (BM + BN) * 128;
+  static_assert(STAGES >= 2 && STAGES <= 4 && BM % 64 == 0 && BN % 64 == 0 && BN / WN <= 128 && 128 % (BN / WN) == 0 && NT % 2 == 0, "");
+  // the results of 32 rows of each wavefront go where the tiles but the first are
+  constexpr int PITCH = BN / WN * sizeof(O), REST = (STAGES - 1) * STAGE, SECOND = REST > 4 * 32 * PITCH ? REST : 4 * 32 * PITCH;
+  constexpr int SCALES = STAGE + SECOND;   // two times four blocks' scales of a
+  __shared__ __attribute__((aligned(128))) uint8_t tiles[SCALES + 2 * BM * 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
   const uint32_t pitch = (uint32_t)g.steps * 128,
-                 lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)all_tiles + group * GROUP;
-  const int turns = (g.steps + SPLIT - 1) / SPLIT;
-  auto block_of = [&](int s) { return s * SPLIT + group; };   // of turn s
+                 lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)tiles;
   const int n_tiles = g.tiles_m * g.tiles_n, xcd = blockIdx.x & 7;
   const int end = (int)((int64_t)n_tiles * (xcd + 1) >> 3);
   int t = (int)((int64_t)n_tiles * xcd >> 3) + (blockIdx.x >> 3);
@@ -292,13 +300,13 @@ __global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
   auto copy_one = [&](int s, int c) {
     const bool of_a = c * 32 < BM;
     copy_1kb(of_a ? a_rows : b_rows, of_a ? from_a : from_b,
-             block_of(s) < g.steps ? (of_a ? c : c - BM / 32) * 32 * pitch + block_of(s) * 128 : 0x80000000u,   // past the end: outside
-             lds0 + (s & 1) * STAGE + (c * 4 + wave) * 1024);
+             s < g.steps ? (of_a ? c : c - BM / 32) * 32 * pitch + s * 128 : 0x80000000u,   // past the end: outside
+             lds0 + (uint32_t)s % STAGES * STAGE + (c * 4 + wave) * 1024);
   };
   auto copy_scales = [&](int s) {
-    const int k = min(block_of(s), g.steps - 1);   // blocks past the end are zeros, times a scale that has to be a number: the last one's
-    copy_256b(s % (4 / SPLIT) == 0 && wave < BM / 64, s0 + (k & ~3), scale_from,
-              lds0 + STAGE + SECOND + (k >> 2 & 1) * BM * 4 + wave % (BM / 64) * 256);
+    const int k = min(s, g.steps - 1);
+    copy_256b(s % 4 == 0 && wave < BM / 64, s0 + (k & ~3), scale_from,
+              lds0 + SCALES + (k >> 2 & 1) * BM * 4 + wave % (BM / 64) * 256);
   };
 
   f32x16 acc[MT][NT];
@@ -310,13 +318,13 @@ __global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
     constexpr int H = decltype(half)::value, R = decltype(index)::value;
     constexpr bool OF_A = R >= 1 && R <= MT;
     constexpr int I = OF_A ? R - 1 : 0, J = R == 0 || OF_A ? 0 : R - MT;
-    const uint8_t* p = tiles + (s & 1) * STAGE + H * 512 + (OF_A ? at_a + I * 4096 : at_b + (J >> 1) * 8192 + (J & 1) * 256);
+    const uint8_t* p = tiles + (uint32_t)s % STAGES * STAGE + H * 512 + (OF_A ? at_a + I * 4096 : at_b + (J >> 1) * 8192 + (J & 1) * 256);
     const uint4 v[2] = {*(const uint4*)(p + (piece ^ turn)), *(const uint4*)(p + ((piece + 16) ^ turn))};
     __builtin_memcpy(OF_A ? &fa[H][I].v : &fb[H][J].v, v, 32);
   };
   auto read_scales = [&](int s) {
-    const int k = min(block_of(s), g.steps - 1);
-    const uint8_t* sa = tiles + STAGE + SECOND + ((k >> 2 & 1) * BM + ra) * 4 + (k & 3);
+    const int k = min(s, g.steps - 1);
+    const uint8_t* sa = tiles + SCALES + ((k >> 2 & 1) * BM + ra) * 4 + (k & 3);
 #pragma unroll
     for (int i = 0; i < MT; ++i) scale_a[i] = sa[128 * i];
     scale_b = sb[k >> 2] >> (k & 3) * 8;
@@ -325,7 +333,7 @@ __global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
   constexpr integral_constant<int, 0> n0;
   constexpr integral_constant<int, 1> n1;
   constexpr int PRODUCTS = MT * NT, READS = MT + NT;
-  // Multiplies block s.  Between the products are the reads of the next half and the copies of the block after the next.  (Left alone,
+  // Multiplies block s.  Between the products are the reads of the next half and the copies of the block STAGES on.  (Left alone,
   // the compiler reads after the products and waits; all reads and copies before them leave the matrix core without work meanwhile:
   // 8192 x 8192 x 8192 585 -> 445 us.)  What is read and copied behind the last block is not used and not fetched: other code there
   // would cost more, in moves between registers.
@@ -341,8 +349,9 @@ __global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
       });
       __builtin_amdgcn_sched_barrier(0);
     });
-    // this wavefront's copies of the next block are done, and its reads of this one; then everybody's are
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    // this wavefront's copies of the next block are done (those of later blocks may be on their way), and its reads of this one;
+    // then everybody's are
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((STAGES - 2) * COPIES) : "memory");
     read_scales(s + 1);
     __builtin_amdgcn_sched_barrier(0);
     each<PRODUCTS>([&](auto index) {
@@ -352,9 +361,9 @@ __global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
         if constexpr (decltype(r)::value * (PRODUCTS - 1) / READS == N) read_one(s + 1, n0, r);
       });
       each<COPIES>([&](auto c) {
-        if constexpr (decltype(c)::value * PRODUCTS / COPIES == N) copy_one(s + 2, decltype(c)::value);
+        if constexpr (decltype(c)::value * PRODUCTS / COPIES == N) copy_one(s + STAGES, decltype(c)::value);
       });
-      if constexpr (N == PRODUCTS - 1) copy_scales(s + 2);
+      if constexpr (N == PRODUCTS - 1) copy_scales(s + STAGES);
       __builtin_amdgcn_sched_barrier(0);
     });
   };
@@ -365,7 +374,7 @@ __global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
   constexpr int COLS = BN / WN, PIECES = PITCH / 16, FIT = SECOND / 4 / PITCH / 32 * 32,
                 ROWS = FIT < MT * 32 ? FIT : MT * 32, AT_ONCE = 64 / PIECES;   // rows that a store takes
   constexpr int STORES = MT * 32 / AT_ONCE;
-  static_assert(ROWS >= 32 && MT * 32 % ROWS == 0 && PIECES <= 64 && COPIES + STORES <= 63, "");
+  static_assert(ROWS >= 32 && MT * 32 % ROWS == 0 && PIECES <= 64 && (STAGES - 1) * COPIES + STORES <= 63, "");
   auto store_results = [&](int64_t row0, int col0, int rows, int cols) {
     uint8_t* room = tiles + STAGE + wave * (SECOND / 4);
     const int out_col = col0 + wn * COLS, left = g.n - out_col;
@@ -425,9 +434,9 @@ __global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
   copy_scales(0);
   bool stores_under_way = false;
   for (;;) {
-    each<COPIES>([&](auto c) { copy_one(1, decltype(c)::value); });
-    if (stores_under_way) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(COPIES + STORES) : "memory");   // they are behind block 0
-    else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(COPIES) : "memory");
+    each<(STAGES - 1) * COPIES>([&](auto c) { copy_one(1 + decltype(c)::value / COPIES, decltype(c)::value % COPIES); });
+    if (stores_under_way) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((STAGES - 1) * COPIES + STORES) : "memory");   // they are behind block 0
+    else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((STAGES - 1) * COPIES) : "memory");
     sb = (const __attribute__((address_space(4))) uint32_t*)uniform(g.b_scale + (size_t)((col0 + min(wn * (BN / WN), cols - 1)) >> 7) * g.quads * 4);
     each<READS>([&](auto r) { read_one(0, n0, r); });
     read_scales(0);
@@ -435,25 +444,9 @@ __global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j) acc[i][j] = 0.f;
-    for (int s = 0; s < turns; ++s) block(s);
+    for (int s = 0; s < g.steps; ++s) block(s);
     // everybody has read the last fragments, and nothing is on its way to LDS
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-    if constexpr (SPLIT == 2) {   // the second group's sums over its own tiles, 4 bytes a lane next to each other
-      float* sums = (float*)(all_tiles + GROUP) + threadIdx.x % 256;
-      static_assert(MT * NT * 16 * 256 * 4 <= GROUP, "");
-      each<MT * NT * 16>([&](auto index) {
-        constexpr int N = decltype(index)::value;
-        if (group == 1) sums[N * 256] = acc[N / 16 % MT][N / 16 / MT][N % 16];
-      });
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
-      if (group == 1) return;   // a workgroup makes one tile then
-      each<MT * NT * 16>([&](auto index) {
-        constexpr int N = decltype(index)::value;
-        acc[N / 16 % MT][N / 16 / MT][N % 16] += sums[N * 256];
-      });
-      store_results(row0, col0, rows, cols);
-      return;
-    }
     const int64_t row = row0;
     const int col = col0, height = rows, width = cols;
     t += gridDim.x >> 3;
@@ -471,38 +464,44 @@ __global__ __launch_bounds__(256 * SPLIT) void matmul_kernel(MatmulArgs g) {
 
 // per_cu: workgroups that a compute unit holds, by LDS.  A workgroup makes several tiles, so that the first block of the next one is on its
 // way while the results of the last one are stored.
-template <typename O, bool EXACT, int BM, int BN, int WM, int WN, int SPLIT>
+template <typename O, bool EXACT, int BM, int BN, int STAGES>
 int run_tiles(MatmulArgs g, int per_cu, hipStream_t st) {
   g.tiles_m = (int)((g.m + BM - 1) / BM);
   g.tiles_n = (g.n + BN - 1) / BN;
   const int tiles = (g.tiles_m * g.tiles_n + 7) / 8 * 8;
-  matmul_kernel<O, EXACT, BM, BN, WM, WN, SPLIT><<<SPLIT == 1 ? std::min(tiles, 256 * per_cu) : tiles, 256 * SPLIT, 0, st>>>(g);
+  matmul_kernel<O, EXACT, BM, BN, STAGES><<<std::min(tiles, 256 * per_cu), 256, 0, st>>>(g);
   return status();
 }
 
-template <typename O, bool EXACT>
+template <typename O, bool EXACT, int R>
 int run_rows(const MatmulArgs& g, hipStream_t st) {
-  matmul_rows_kernel<O, EXACT><<<(g.n + 15) / 16, 512, 0, st>>>(g);
+  matmul_rows_kernel<O, EXACT, R><<<(g.n + 15) / 16, 512, 0, st>>>(g);
   return status();
 }
 
 template <typename O, bool EXACT>
 int run_matmul(const MatmulArgs& g, hipStream_t st) {
-  if (g.m <= 16) return run_rows<O, EXACT>(g, st);
-  // Tiles of 256 x 256 read each row of either operand half as often as those of 128 x 128, a round of them (one a compute unit) takes 1.45 times
-  // as long as a round of the others (two a unit).  us, 256 -> 128: 1500 x 5120 x 5120 (120 tiles, one round each) 55.5 -> 40.7; 2048 (1 and
-  // 2 rounds) 58.2 -> 71.5; 3000 (1 and 2) 65.7 -> 79.1; 4096 (2 and 3) 118.1 -> 113.5; 33272 x 15360 (31 and 61) 2144 -> 2603.
-  // 64 x 128 where 128 x 128 would leave units idle, in two groups while there are fewer tiles than units.  us, 128 -> 64 -> 64 in groups:
-  // 64 x 5120 x 5120 (40 tiles of 64 x 128) 23.0 -> 19.0 -> 15.3; 256 (160) 33.6 -> 26.5 -> 21.9; 512 (320) 33.8 -> 28.7 -> 40.7; 1024 (640)
-  // 36.3 -> 40.5 -> 61.5; 2500 x 1536 x 1536 (480) 10.6 -> 10.7 -> 14.4.
-  // Up to 16 rows without tiles.  us, rows -> 64 x 128 in groups: 16 x 5120 x 5120 11.5 -> 14.9; 32 16.4 -> 15.1; 48 23.7 -> 15.2.
   auto tiles = [&](int bm, int bn) { return (g.m + bm - 1) / bm * ((g.n + bn - 1) / bn); };
   auto rounds = [&](int64_t n, int at_once) { return (n + at_once - 1) / at_once; };
+  // Figures in us, with weights that no cache holds but where 256 x 256 is compared.
+  // Up to 16 rows without tiles, up to 32 where their second reading by each 16 columns is short.  Rows -> 64 x 128: 16 x 5120 x 5120
+  // 12.9 -> 20.8; 16 x 15360 24.0 -> 23.3; 20 x 1536 x 1536 6.8 -> 8.0; 20 x 5120 x 5120 16.4 -> 21.1; 32 19.1 -> 22.4; 32 x 9216 x 1536
+  // 11.7 -> 9.5; 48 x 5120 x 5120 (three times 16) 24.8 -> 23.7.
+  if (g.m <= 16) return run_rows<O, EXACT, 1>(g, st);
+  if (g.m <= 32 && g.n <= 6144) return run_rows<O, EXACT, 2>(g, st);
+  // Tiles of 256 x 256 read each row of either operand half as often as those of 128 x 128, a round of them (one a compute unit) takes 1.45
+  // times as long as a round of the others (two a unit).  256 -> 128: 1500 x 5120 x 5120 (120 tiles, one round each) 55.5 -> 40.7; 2048 (1
+  // and 2 rounds) 58.2 -> 71.5; 3000 (1 and 2) 65.7 -> 79.1; 4096 (2 and 3) 118.1 -> 113.5; 33272 x 15360 (31 and 61) 2144 -> 2603.
   if constexpr (!EXACT)
-    if (1.45 * rounds(tiles(256, 256), 256) <= rounds(tiles(128, 128), 512)) return run_tiles<O, EXACT, 256, 256, 2, 2, 1>(g, 1, st);
-  if (tiles(64, 128) <= 256) return run_tiles<O, EXACT, 64, 128, 2, 2, 2>(g, 1, st);
-  if (tiles(64, 128) <= 512) return run_tiles<O, EXACT, 64, 128, 2, 2, 1>(g, 2, st);
-  return run_tiles<O, EXACT, 128, 128, 2, 2, 1>(g, 2, st);
+    if (1.45 * rounds(tiles(256, 256), 256) <= rounds(tiles(128, 128), 512)) return run_tiles<O, EXACT, 256, 256, 2>(g, 1, st);
+  // No more tiles than units: one a unit, four LDS tiles deep, which is what hides the memory's latency then (two -> three -> four -> five ->
+  // six deep: 64 x 5120 x 5120 40.2 -> 29.5 -> 25.4 -> 25.9 -> 26.2).  64 x 128, or 128 x 128 where the former are more than units.  64 x 128
+  // two deep, two a unit -> four deep -> 128 x 128 four deep: 256 x 5120 x 5120 (160 and 80) 36.9 -> 23.5 -> 31.4; 400 (280 and 160) 36.9 ->
+  // 37.6 -> 29.1; 900 x 4096 x 4096 (480 and 256) 31.4 -> 32.0 -> 24.1; float32 200 x 5120 x 5120 41.9 -> 31.2 -> 41.6, 900 x 4096 x 4096
+  // 41.7 -> 50.9 -> 40.2.
+  if (tiles(64, 128) <= 256) return run_tiles<O, EXACT, 64, 128, 4>(g, 1, st);
+  if (tiles(128, 128) <= 256) return run_tiles<O, EXACT, 128, 128, 4>(g, 1, st);
+  return run_tiles<O, EXACT, 128, 128, 2>(g, 2, st);
 }
 
 template <typename X>
