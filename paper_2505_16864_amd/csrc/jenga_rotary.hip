@@ -55,6 +55,12 @@ __device__ __forceinline__ Pair pair_of(const Turns& t, int c, int* other, bool*
   return p;
 }
 
+// Halves paired: the first channel of pair p of a head; behind the axes the channels 2 p of neighbours that stay.
+__device__ __forceinline__ int first_of_pair(const Turns& t, int p) {
+  const int e0 = t.pairs[0], e1 = e0 + t.pairs[1], e2 = e1 + t.pairs[2];
+  return p < e0 ? p : p < e1 ? p + e0 : p < e2 ? p + e1 : 2 * p;
+}
+
 // cos and sin for a pair of a token in these cells; false: the pair stays as it is, to the last bit.
 __device__ __forceinline__ bool turn_of(const Turns& t, const Pair& p, const int cell[3], float2* turn) {
   const int n = p.axis == 0 ? cell[0] : p.axis == 1 ? cell[1] : cell[2];
@@ -191,18 +197,14 @@ __global__ __launch_bounds__(256) void rotary_pairs_kernel(RotaryArgs a) {
   if (unit >= a.units) return;
   const int p = (int)(id - unit * (uint32_t)half);
   const int64_t b = unit / a.tokens, n = unit % a.tokens;
-  int c0 = 2 * p, c1 = 2 * p + 1;
-  if (HALVES) {   // pair p of the axis it falls on; behind the axes neighbours
-    const int e0 = a.turns.pairs[0], e1 = e0 + a.turns.pairs[1], e2 = e1 + a.turns.pairs[2];
-    if (p < e0) c0 = p, c1 = p + a.turns.pairs[0];
-    else if (p < e1) c0 = p + e0, c1 = c0 + a.turns.pairs[1];
-    else if (p < e2) c0 = p + e1, c1 = c0 + a.turns.pairs[2];
-  }
   int cell[3], other;
   bool second;
   cells_of(a, unit, n, cell);
   float2 t;
-  const bool turned = turn_of(a.turns, pair_of<HALVES>(a.turns, c0, &other, &second), cell, &t);
+  const int c0 = HALVES ? first_of_pair(a.turns, p) : 2 * p;
+  const Pair pair = pair_of<HALVES>(a.turns, c0, &other, &second);
+  const int c1 = pair.axis == 3 ? c0 + 1 : other;
+  const bool turned = turn_of(a.turns, pair, cell, &t);
   const int h0 = blockIdx.y * a.heads_per_wg;
   for (int k = 0; k < a.count; ++k) {
     const X* src = (const X*)a.src[k] + b * a.src_batch[k] + n * a.src_token[k];
@@ -284,37 +286,45 @@ __global__ __launch_bounds__(256) void permute_turn_pool_kernel(TurnedMoves move
     if (s[u] >= 0) v[u] = *(const Piece16*)(src + (size_t)s[u] * moves.token);
   }
   if (tensor < 2 && j < M_v) {   // blocks of vision tokens hold no text
-    constexpr int N = HALVES ? 8 : 4;
-    Pair pair[N];
-    int other[N];
-    bool second[N];
+    // The thread's four pairs of each row: of its piece, or, halves paired, those CH apart, so that the lanes of a row read neighbouring
+    // angles; they take both channels from LDS then and put them back.
+    Pair pair[4];
+    int first[4], other[4];
+    bool second;
 #pragma unroll
-    for (int i = 0; i < N; ++i) pair[i] = pair_of<HALVES>(turns, c * 8 + (HALVES ? i : 2 * i), &other[i], &second[i]);
+    for (int i = 0; i < 4; ++i) {
+      first[i] = HALVES ? first_of_pair(turns, c + i * CH) : c * 8 + 2 * i;
+      pair[i] = pair_of<HALVES>(turns, first[i], &other[i], &second);
+    }
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
       int cell[3] = {-1, -1, -1};
       if (s[u] >= 0) turns.grid.split((uint32_t)s[u], cell);
-      f32x8 f = Eight<__bf16>::wide(v[u]);
       float2 t;
       if (HALVES) {
-        __builtin_memcpy(&room[threadIdx.x * 8], &v[u], 16);
+        __bf16* row = room + g * D;
+        __builtin_memcpy(row + c * 8, &v[u], 16);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // a row is 8 or 16 lanes of one wavefront
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float y = (float)room[g * D + other[i]];
-          if (turn_of(turns, pair[i], cell, &t)) f[i] = fmaf(f[i], t.x, second[i] ? y * t.y : -(y * t.y));
+        for (int i = 0; i < 4; ++i) {
+          if (!turn_of(turns, pair[i], cell, &t)) continue;
+          const float x = (float)row[first[i]], y = (float)row[other[i]];
+          row[first[i]] = (__bf16)fmaf(x, t.x, -(y * t.y));
+          row[other[i]] = (__bf16)fmaf(y, t.x, x * t.y);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+        __builtin_memcpy(&v[u], row + c * 8, 16);
       } else {
+        f32x8 f = Eight<__bf16>::wide(v[u]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
+        for (int i = 0; i < 4; ++i) {
           const float x = f[2 * i], y = f[2 * i + 1];
           if (turn_of(turns, pair[i], cell, &t)) f[2 * i] = fmaf(x, t.x, -(y * t.y)), f[2 * i + 1] = fmaf(x, t.y, y * t.x);
         }
+        v[u] = Eight<__bf16>::narrow(f);
       }
-      v[u] = Eight<__bf16>::narrow(f);
     }
   }
 #pragma unroll
