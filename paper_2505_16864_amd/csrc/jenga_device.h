@@ -156,7 +156,12 @@ __device__ __forceinline__ uint2 to_e4m3(const f32x8& v, float inverse) {
 __device__ __forceinline__ float largest_of(const f32x8& v) {
   float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_magnitude(v[i]));
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(v[i]));   // NaN loses
+  if (m == __builtin_inff()) {
+    m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_magnitude(v[i]));
+  }
   return m;
 }
 

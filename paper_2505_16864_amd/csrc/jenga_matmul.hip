@@ -25,6 +25,7 @@ int status() { return hipGetLastError() == hipSuccess ? JENGA_OK : JENGA_EHIP; }
 // ---- quantisation: bound by memory
 
 // A scale for each row and 128 columns: 16 lanes hold a block, a wavefront four, which is what a group of four scale bytes is for.
+// 33272 x 5120 bf16: 89 us, 5.7 TB/s.
 template <typename X>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const X* __restrict__ x, int64_t x_stride, uint8_t* __restrict__ q,
                                                             uint8_t* __restrict__ scale, int64_t units, int cols, int quads) {
@@ -250,6 +251,11 @@ __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int* tm
 // into one of STAGES LDS tiles while another is multiplied; within a block the products of one half of the columns run while the
 // fragments of the next half are read into registers.  So the reads of an LDS tile end in the middle of its block, and that is where
 // the barrier is: behind it the next tile is complete, and the one STAGES blocks on goes over this one.
+//
+// 33272 x 15360 x 5120 to bf16: 1.95 to 2.0 ms, 2.65 to 2.69 PFLOP/s, where the library's product with one scale for each operand takes
+// 1.84 to 1.97; the matrix cores are busy 70 % of the cycles at the 1.67 GHz that the package power leaves (all-zero operands: 1.77 ms), no
+// bank conflicts.  Float32 results, through the bf16 matrix core: 1.15 PFLOP/s.  16 x 16 x 128 products, eight wavefronts, results in
+// LDS room of their own and wider or narrower stripes were slower or the same.
 //
 // A copy instruction takes 8 whole rows of 128 bytes: first their left halves, then the right ones.  The 16-byte pieces of a half row are
 // rotated by an exclusive or with bits of the row, so that the rows of a fragment fall on all banks.  The rows of b are the rows of

@@ -2,7 +2,8 @@
 //
 // Pair i of an axis with d channels turns by the angle (origin + step * cell) * theta^(-2i/d); cos and sin of every pair and cell come
 // from a table of T d_t + H d_h + W d_w floats that stays in the caches, so the tensors themselves are what is moved: bound by memory.
-// A thread keeps the angles of its channels of one token in registers and walks over the heads.
+// A thread keeps the angles of its channels of one token in registers and walks over the heads.  Q and K of 119056 tokens x 24 heads x 128
+// bf16: 576 us, 5.08 TB/s, either way of pairing; in place 4.9 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -258,7 +259,8 @@ Turns turns_of(const jenga_rotary_config& c, const float* table) {
 // ---- Q, K and V into curve order, Q and K turned on the way, with the block means of Q and K: the first launch of
 // jenga_forward_rotary.  As permute_pool_kernel (jenga_select.hip), a workgroup for a block of one (batch, head), tokens `token` elements
 // apart.  The turn is rounded to bf16 before it is stored and summed, so that the results are those of jenga_rotary and
-// jenga_forward one after the other.
+// jenga_forward one after the other.  Three tensors of 119056 tokens x 24 heads x 128: 1.10 ms, 4.0 TB/s, the lookups of angles; 0.86 without
+// the turn, and 0.58 for a turn by itself.
 struct TurnedMoves {
   const uint16_t* src[3];
   Piece16* dst[3];
