@@ -5,6 +5,7 @@ import of this module fails: there is no fallback.
 """
 import ctypes
 import os
+import struct
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libjenga.so")
@@ -94,14 +95,13 @@ def _load():
     lib.jenga_stage_switch.argtypes = [vp, vp, vp, vp] + [ctypes.c_int32] * 7 + [ctypes.c_float, vp]
     i32, i64, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     lib.jenga_quantize.argtypes = [vp, i64, i32, i64, i32, i32, vp, vp, vp]
-    lib.jenga_matmul.argtypes = [ctypes.POINTER(jenga_matmul_config)] + [vp] * 7
-    norm = ctypes.POINTER(jenga_norm_config)
-    lib.jenga_layer_norm.argtypes = [norm] + [vp] * 8
-    lib.jenga_layer_norm_grad.argtypes = [norm] + [vp] * 9 + [size, vp]
-    lib.jenga_layer_norm_grad_workspace.argtypes = [norm, ctypes.POINTER(ctypes.c_uint64)]
+    # the structs of these calls are passed by address, as ctypes structures or packed
+    lib.jenga_matmul.argtypes = [vp] * 8
+    lib.jenga_layer_norm.argtypes = [vp] * 9
+    lib.jenga_layer_norm_grad.argtypes = [vp] * 10 + [size, vp]
+    lib.jenga_layer_norm_grad_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
     lib.jenga_rotary_table.argtypes = [ctypes.POINTER(jenga_rotary_config), vp]
-    lib.jenga_rotary.argtypes = [ctypes.POINTER(jenga_rotary_config), vp, vp, vp, ctypes.POINTER(jenga_rotary_tensor), i32, i64,
-                                 i64, vp]
+    lib.jenga_rotary.argtypes = [vp] * 5 + [i32, i64, i64, vp]
     lib.jenga_forward_rotary.argtypes = [vp, ctypes.POINTER(jenga_rotary_config)] + [vp] * 4 + [i64] + [vp] * 7 + [size, vp, vp, vp,
                                                                                                                 size, vp, vp]
     lib.jenga_strerror.argtypes = [ctypes.c_int]
@@ -235,6 +235,7 @@ _EINVAL = -1
 _TYPES = {}            # torch's element types to jenga_type, filled by the first call that needs them
 _DTYPE = {}            # and by name
 _current_device = None
+_MATMUL, _NORM, _TENSOR = struct.Struct("=2q4i"), struct.Struct("=5q4i2f"), struct.Struct("=2Q6q2i")   # as the structures above
 
 
 def _use_torch():
@@ -248,6 +249,14 @@ def _use_torch():
 
 def _refuse(what, why):
     raise JengaError(_EINVAL, "%s: %s" % (what, why))
+
+
+def _pack(what, layout, *values):
+    """A structure as bytes: a third of the time that ctypes takes to fill one."""
+    try:
+        return layout.pack(*values)
+    except (struct.error, OverflowError):
+        _refuse(what, "sizes or numbers out of range")
 
 
 def _type(t, what):
@@ -282,9 +291,11 @@ def _matrix(t, what, rows=None, cols=None):
 
 def _whole(t, what, shape, dtype):
     """Refuses anything but a tensor of this shape and type (a name in _DTYPE) without gaps."""
-    if t.shape != shape or t.dtype != _DTYPE[dtype] or not t.is_contiguous():
-        if dtype != "e4m3" or t.dtype != _DTYPE["u8"] or t.shape != shape or not t.is_contiguous():   # its bytes will do
-            _refuse(what, "shape %s, type %s" % (tuple(t.shape), t.dtype))
+    if t.is_contiguous() and t.shape == shape:
+        have = t.dtype
+        if have is _DTYPE[dtype] or (dtype == "e4m3" and have is _DTYPE["u8"]):   # its bytes will do
+            return
+    _refuse(what, "shape %s, type %s" % (tuple(t.shape), t.dtype))
 
 
 def scale_columns(cols):
@@ -307,6 +318,8 @@ def jenga_quantize(x, q, scale, block_rows=1, stream=None):
     _whole(q, what, (rows, padded_columns(cols)), "e4m3")
     _whole(scale, what, (-(-rows // block_rows), scale_columns(cols)), "u8")
     _on_device(what, (x, q, scale))
+    if cols > 0x7FFFFFFF:
+        _refuse(what, "%d columns" % cols)
     if rows:
         _check(_lib.jenga_quantize(x.data_ptr(), stride, kind, rows, cols, block_rows, q.data_ptr(), scale.data_ptr(), stream), what)
 
@@ -327,7 +340,7 @@ def jenga_matmul(a, a_scale, b, b_scale, out, bias=None, stream=None):
         _whole(bias, what, (n,), "f32")
     _on_device(what, (a, a_scale, b, b_scale, out, bias))
     if m:
-        _check(_lib.jenga_matmul(ctypes.byref(jenga_matmul_config(m, stride, n, k, kind, 0)), a.data_ptr(), a_scale.data_ptr(),
+        _check(_lib.jenga_matmul(_pack(what, _MATMUL, m, stride, n, k, kind, 0), a.data_ptr(), a_scale.data_ptr(),
                                  b.data_ptr(), b_scale.data_ptr(), None if bias is None else bias.data_ptr(), out.data_ptr(), stream), what)
 
 
@@ -349,7 +362,7 @@ def _norm_config(what, x, y, weight, bias, group_rows, weight_offset, eps):
                 _refuse(what, "weight and bias differ in stride or type")
             param_stride, param_type = stride, _type(p, what)
     y_stride = _matrix(y, what, rows, cols if y_type != JENGA_E4M3 else padded_columns(cols))
-    return jenga_norm_config(rows, group_rows, x_stride, y_stride, param_stride, cols, x_type, y_type, param_type, eps, weight_offset)
+    return _pack(what, _NORM, rows, group_rows, x_stride, y_stride, param_stride, cols, x_type, y_type, param_type, eps, weight_offset)
 
 
 def jenga_layer_norm(x, y, weight=None, bias=None, y_scale=None, mean=None, rstd=None, group_rows=0, weight_offset=0.0,
@@ -367,7 +380,7 @@ def jenga_layer_norm(x, y, weight=None, bias=None, y_scale=None, mean=None, rstd
         _whole(rstd, what, (rows,), "f32")
     _on_device(what, (x, y, weight, bias, y_scale, mean, rstd))
     if rows:
-        _check(_lib.jenga_layer_norm(ctypes.byref(cfg), x.data_ptr(), None if weight is None else weight.data_ptr(),
+        _check(_lib.jenga_layer_norm(cfg, x.data_ptr(), None if weight is None else weight.data_ptr(),
                                      None if bias is None else bias.data_ptr(), y.data_ptr(),
                                      None if y_scale is None else y_scale.data_ptr(), None if mean is None else mean.data_ptr(),
                                      None if rstd is None else rstd.data_ptr(), stream), what)
@@ -387,13 +400,13 @@ def jenga_layer_norm_grad(x, dy, dx, weight, mean, rstd, dweight=None, dbias=Non
     what = "jenga_layer_norm_grad"
     cfg = _norm_config(what, x, dy, weight, None, group_rows, weight_offset, 0.0)
     rows, cols = x.shape
-    if cfg.y_type != cfg.x_type or dx.dtype != x.dtype or _matrix(dx, what, rows, cols) != cfg.x_stride and rows > 1:
+    if dy.dtype != x.dtype or dx.dtype != x.dtype or _matrix(dx, what, rows, cols) != x.stride(0) and rows > 1:
         _refuse(what, "dy is not of x's type, or dx is not laid out as x is")
     if mean is None or rstd is None:
         _refuse(what, "mean and rstd of the forward pass are wanted")
     _whole(mean, what, (rows,), "f32")
     _whole(rstd, what, (rows,), "f32")
-    groups = -(-rows // cfg.group_rows)
+    groups = -(-rows // (group_rows or rows or 1))
     for t in (dweight, dbias):
         if t is not None:
             if t.numel() != groups * cols:
@@ -401,7 +414,7 @@ def jenga_layer_norm_grad(x, dy, dx, weight, mean, rstd, dweight=None, dbias=Non
             _whole(t, what, t.shape, "f32")
     _on_device(what, (x, dy, dx, weight, mean, rstd, dweight, dbias, workspace))
     if rows:
-        _check(_lib.jenga_layer_norm_grad(ctypes.byref(cfg), x.data_ptr(), dy.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(),
+        _check(_lib.jenga_layer_norm_grad(cfg, x.data_ptr(), dy.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(),
                                           dx.data_ptr(), _ptr(dweight), _ptr(dbias), _ptr(workspace),
                                           0 if workspace is None else workspace.numel() * workspace.element_size(), stream), what)
 
@@ -434,7 +447,7 @@ def _rotary_tensor(cfg, src, dst, what):
         _refuse(what, "shapes %s, %s" % (tuple(shape), tuple(dst.shape)))
     if s[3] != 1 or d[3] != 1 or dst.dtype != src.dtype:
         _refuse(what, "types differ or the channels of a head are not next to each other")
-    return jenga_rotary_tensor(src.data_ptr(), dst.data_ptr(), s[0], s[1], s[2], d[0], d[1], d[2], shape[2], 0)
+    return _pack(what, _TENSOR, src.data_ptr(), dst.data_ptr(), s[0], s[1], s[2], d[0], d[1], d[2], shape[2], 0)
 
 
 def jenga_rotary(cfg, table, q, q_out, k=None, k_out=None, cells=None, plan=None, stream=None):
@@ -445,9 +458,9 @@ def jenga_rotary(cfg, table, q, q_out, k=None, k_out=None, cells=None, plan=None
     if (k is None) != (k_out is None):
         _refuse(what, "k without k_out, or the other way round")
     if k is None:
-        tensors = (jenga_rotary_tensor * 1)(_rotary_tensor(cfg, q, q_out, what))
+        tensors = _rotary_tensor(cfg, q, q_out, what)
     else:
-        tensors = (jenga_rotary_tensor * 2)(_rotary_tensor(cfg, q, q_out, what), _rotary_tensor(cfg, k, k_out, what))
+        tensors = _rotary_tensor(cfg, q, q_out, what) + _rotary_tensor(cfg, k, k_out, what)
         if k.dtype != q.dtype or k.shape[:2] != q.shape[:2]:
             _refuse(what, "q and k differ in type or tokens")
     batch, tokens = q.shape[0], q.shape[1]
@@ -456,10 +469,11 @@ def jenga_rotary(cfg, table, q, q_out, k=None, k_out=None, cells=None, plan=None
         _whole(cells, what, (batch, tokens, 3), "i32")
     _on_device(what, (q, q_out, k, k_out, table, cells))
     if batch and tokens:
-        mine = jenga_rotary_config.from_buffer_copy(cfg)
-        mine.type = kind
-        _check(_lib.jenga_rotary(ctypes.byref(mine), plan, None if cells is None else cells.data_ptr(), table.data_ptr(), tensors,
-                                 len(tensors), batch, tokens, stream), what)
+        if cfg.type != kind:
+            cfg = jenga_rotary_config.from_buffer_copy(cfg)
+            cfg.type = kind
+        _check(_lib.jenga_rotary(ctypes.byref(cfg), plan, None if cells is None else cells.data_ptr(), table.data_ptr(), tensors,
+                                 1 if k is None else 2, batch, tokens, stream), what)
 
 
 def jenga_forward_rotary(plan, cfg, table, q_thw, k_thw, v_thw, q_curve, k_curve, v_curve, sel_count, sel_index, mask,

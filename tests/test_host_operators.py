@@ -241,3 +241,12 @@ def test_rotary_table_refuses_angles_that_are_not_finite(bad):
     with pytest.raises(J.JengaError) as e:
         J.jenga_rotary_table(cfg, np.zeros(3 * 4 + 4 * 2 + 5 * 6, dtype=np.float32))
     assert e.value.status == EINVAL
+
+
+def test_the_binding_refuses_numbers_that_do_not_fit():
+    x, y = torch.zeros(4, 64), torch.zeros(4, 64)
+    for call in (lambda: J.jenga_layer_norm(x, y, eps=1e300), lambda: J.jenga_layer_norm(x, y, weight_offset=-1e300),
+                 lambda: J.jenga_layer_norm(x, y, group_rows=1 << 70)):
+        with pytest.raises(J.JengaError) as e:
+            call()
+        assert e.value.status == EINVAL
