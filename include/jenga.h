@@ -381,6 +381,8 @@ int jenga_layer_norm_grad_workspace(const jenga_norm_config* cfg, uint64_t* byte
  * Rotary positions over the axes of a T x H x W grid.  The first dim[0] channels of a head turn with the token's
  * t, the next dim[1] with its h, the next dim[2] with its w, the rest stay as they are.  Pair i of an axis with d
  * channels turns by (origin + step * cell) * theta^(-2i / d):  (x, y) -> (x cos - y sin, x sin + y cos).
+ * JENGA_EUNSUPPORTED, in all calls with such a config: more than 2^24 cells, an odd head_dim or one above 1024, more than
+ * 2^31 - 1024 pairs of all axes and cells, (T dim[0] + H dim[1] + W dim[2]) / 2.
  */
 enum {
   JENGA_ROTARY_HALVES = 1u, /* pair i of an axis is its channels i and i + d/2; else 2i and 2i + 1   */

@@ -223,6 +223,8 @@ int rotary_config_ok(const jenga_rotary_config* c) {
   const int64_t lim = 1ll << 24;
   if (c->head_dim % 2 != 0 || c->head_dim > 1024) return JENGA_EUNSUPPORTED;
   if (c->T > lim || c->H > lim || c->W > lim || (int64_t)c->T * c->H > lim || (int64_t)c->T * c->H * c->W > lim) return JENGA_EUNSUPPORTED;
+  // the kernels' places in the table are 32-bit numbers: all its pairs, and up to 1023 that no axis has behind them
+  if (((int64_t)c->T * c->dim[0] + (int64_t)c->H * c->dim[1] + (int64_t)c->W * c->dim[2]) / 2 > (1ll << 31) - 1024) return JENGA_EUNSUPPORTED;
   return JENGA_OK;
 }
 

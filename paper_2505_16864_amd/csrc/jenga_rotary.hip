@@ -37,7 +37,8 @@ struct RotaryArgs {
   int heads_per_wg;
 };
 
-// A pair's place: its axis (3: none, it stays) and where cell 0 of it is in the table.
+// A pair's place: its axis (3: none, it stays) and where cell 0 of it is in the table.  The checks of arguments hold the pairs of all
+// cells below 2^31 - 1024, so that 32 bits take any place.
 struct Pair {
   int axis, at, step;
 };
