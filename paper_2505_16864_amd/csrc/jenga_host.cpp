@@ -5,7 +5,6 @@
 #include <cmath>
 #include <cstring>
 #include <new>
-#include <utility>
 
 #include "jenga_internal.h"
 
@@ -238,23 +237,6 @@ struct Layout4 {
   int64_t width, size;          // head_dim, bytes of an element
   int64_t end() const { return (n[0] - 1) * batch + (n[1] - 1) * token + (n[2] - 1) * head + width; }
 
-  // No two elements in one place: each stride, from the smallest on, steps over all that the smaller ones reach.
-  bool distinct() const {
-    int64_t stride[3] = {batch, token, head}, count[3] = {n[0], n[1], n[2]};
-    int64_t reach = width;
-    for (int left = 3; left > 0; --left) {
-      int best = 0;
-      for (int i = 1; i < left; ++i)
-        if (count[best] == 1 || (count[i] > 1 && stride[i] < stride[best])) best = i;
-      if (count[best] > 1) {
-        if (stride[best] < reach) return false;
-        reach += (count[best] - 1) * stride[best];
-      }
-      std::swap(stride[best], stride[left - 1]);
-      std::swap(count[best], count[left - 1]);
-    }
-    return true;
-  }
   // The same bytes as rows of a common pitch, where the heads of a token lie within one token stride.
   Span rows() const {
     const int64_t row = (n[2] - 1) * head + width;
@@ -263,6 +245,73 @@ struct Layout4 {
     return {at, 1, end() * size, end() * size};
   }
 };
+
+// The steps of two tensors along one axis.
+struct Axis {
+  int64_t stride, a, b;       // entries of either tensor
+  int64_t reach_a, reach_b;   // elements from the first to behind the last one of all axes behind this one
+};
+constexpr int MOST_STEPS = 16;
+
+// Whether steps along the axes bring rows of `width` elements over each other that start `apart` elements from each other.  Steps of an outer
+// axis leave few distances that the inner ones can bridge, two at most where strides are nested; more than MOST_STEPS are not looked
+// through, which refuses a call rather than take a wrong one.
+bool meet(const Axis* axis, int axes, __int128 apart, int64_t width) {
+  if (axes == 0) return apart < width && -apart < width;
+  const __int128 s = axis->stride, from = apart - axis->reach_a, to = apart + axis->reach_b;   // wanted: t with from < s t < to
+  auto floor_div = [](__int128 x, __int128 y) { return x / y - (x % y != 0 && x < 0); };
+  const __int128 first = std::max<__int128>(floor_div(from, s) + 1, 1 - (__int128)axis->b);
+  const __int128 last = std::min<__int128>(-floor_div(-to, s) - 1, (__int128)axis->a - 1);
+  if (last - first >= MOST_STEPS) return true;
+  for (__int128 t = first; t <= last; ++t)
+    if (meet(axis + 1, axes - 1, apart - s * t, width)) return true;
+  return false;
+}
+
+// The axes of two tensors, the outermost first, without those along which there is nothing to step; -1: their strides differ.
+int common_axes(const Layout4& a, const Layout4& b, Axis axis[3]) {
+  const int64_t of_a[3] = {a.batch, a.token, a.head}, of_b[3] = {b.batch, b.token, b.head};
+  int axes = 0;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t na = of_a[i] == 0 ? 1 : a.n[i], nb = of_b[i] == 0 ? 1 : b.n[i];   // stride 0: all in one place
+    if (na == 1 && nb == 1) continue;
+    if (na > 1 && nb > 1 && of_a[i] != of_b[i]) return -1;
+    axis[axes++] = {na > 1 ? of_a[i] : of_b[i], na, nb, 0, 0};
+  }
+  std::sort(axis, axis + axes, [](const Axis& x, const Axis& y) { return x.stride > y.stride; });
+  int64_t reach_a = a.width, reach_b = b.width;
+  for (int i = axes - 1; i >= 0; --i) {
+    axis[i].reach_a = reach_a;
+    axis[i].reach_b = reach_b;
+    reach_a += (axis[i].a - 1) * axis[i].stride;
+    reach_b += (axis[i].b - 1) * axis[i].stride;
+  }
+  return axes;
+}
+
+// Whether two tensors may share an element: not where they are rows of a common pitch that lie between each other's, nor where they have
+// the same strides and no steps of them lead from the one to the other.
+bool share(const Layout4& a, const Layout4& b) {
+  if (!overlap(a.rows(), b.rows())) return false;
+  Axis axis[3];
+  const int axes = common_axes(a, b, axis);
+  return axes < 0 || meet(axis, axes, ((__int128)(uintptr_t)b.at - (__int128)(uintptr_t)a.at) / a.size, a.width);
+}
+
+// No two elements of a tensor in one place: no steps along an axis that those along the smaller strides undo.
+bool distinct(const Layout4& a) {
+  for (int i = 0; i < 3; ++i)
+    if (a.n[i] > 1 && (i == 0 ? a.batch : i == 1 ? a.token : a.head) == 0) return false;
+  Axis axis[3];
+  const int axes = common_axes(a, a, axis);
+  for (int i = 0; i < axes; ++i) {
+    const int64_t most = std::min(axis[i].a - 1, (axis[i].reach_a - 1) / axis[i].stride);   // further ones are behind all of them
+    if (most > MOST_STEPS) return false;
+    for (int64_t t = 1; t <= most; ++t)
+      if (meet(axis + i + 1, axes - i - 1, (__int128)t * axis[i].stride, a.width)) return false;
+  }
+  return true;
+}
 
 }  // namespace
 
@@ -293,7 +342,7 @@ int rotary_args_ok(const jenga_rotary_config* c, const jenga_plan* plan, const i
       return JENGA_EUNSUPPORTED;
     src[i] = {t.src, t.src_batch, t.src_token, t.src_head, {batch, tokens, t.heads}, c->head_dim, size};
     dst[i] = {t.dst, t.dst_batch, t.dst_token, t.dst_head, {batch, tokens, t.heads}, c->head_dim, size};
-    if (!dst[i].distinct()) return JENGA_EINVAL;
+    if (!distinct(dst[i])) return JENGA_EINVAL;
   }
   if (batch == 0 || tokens == 0) return JENGA_OK;
   const int64_t n_table = (int64_t)c->T * c->dim[0] + (int64_t)c->H * c->dim[1] + (int64_t)c->W * c->dim[2];
@@ -304,8 +353,8 @@ int rotary_args_ok(const jenga_rotary_config* c, const jenga_plan* plan, const i
     for (int j = 0; j < count; ++j) {
       const bool in_place = i == j && src[i].at == dst[i].at && (batch == 1 || src[i].batch == dst[i].batch) &&
                             (tokens == 1 || src[i].token == dst[i].token) && (tensors[i].heads == 1 || src[i].head == dst[i].head);
-      if (!in_place && overlap(to, src[j].rows())) return JENGA_EINVAL;
-      if (j < i && overlap(to, dst[j].rows())) return JENGA_EINVAL;
+      if (!in_place && share(dst[i], src[j])) return JENGA_EINVAL;
+      if (j < i && share(dst[i], dst[j])) return JENGA_EINVAL;
     }
   }
   return JENGA_OK;

@@ -63,3 +63,63 @@ def test_the_library_refuses_them(grid, head_dim, dims):
     for n, v in dict(src=4 * A, dst=12 * A, src_token=head_dim, src_head=head_dim, dst_token=head_dim, dst_head=head_dim, heads=1).items():
         setattr(list_[0], n, v)
     assert J.raw().jenga_rotary(ctypes.byref(cfg), None, None, A, list_, 1, 1, 0, None) == EUNSUPPORTED   # no tokens: nothing to launch
+
+
+GRID, D, DIMS = (2, 4, 5), 8, (2, 2, 4)
+
+
+def _in_place(batch, tokens, heads, starts, strides):
+    """One or two tensors turned in place, `starts` elements behind A."""
+    return GRID, D, DIMS, batch, tokens, [(A + 2 * s, A + 2 * s, heads, strides, strides) for s in starts]
+
+
+# Q and K as columns of one projection [batch, tokens, 3, heads, D], from one token of each sequence on; head by head
+# [batch, 3, heads, tokens, D]; heads of Q and K in turn.
+@pytest.mark.parametrize("batch,tokens", [(1, 1), (2, 1), (7, 1), (1, 2), (2, 2), (3, 33)])
+def test_interleaved_tensors_are_apart(driver, batch, tokens):
+    heads = 3
+    row = heads * D
+    for strides, k in (((tokens * 3 * row, 3 * row, D), row), ((tokens * 3 * row, 3 * row, D), 2 * row),
+                       ((3 * heads * tokens * D, D, tokens * D), heads * tokens * D),
+                       ((tokens * 2 * row, 2 * row, 2 * D), D), ((D, 2 * batch * D, 2 * tokens * batch * D), batch * D),
+                       ((row, 2 * batch * row, D), batch * row)):
+        assert _statuses(driver, [_in_place(batch, tokens, heads, (0, k), strides), _in_place(batch, tokens, heads, (k, 0), strides)]) == \
+            [OK, OK], strides
+        # where they do share something: half of a head, and the next heads' or rows'
+        bad = [_in_place(batch, tokens, heads, (0, k + D // 2), strides)] if k == D else [_in_place(batch, tokens, heads, (0, D // 2), strides)]
+        assert _statuses(driver, bad) == [EINVAL], strides
+
+
+def _places(start, batch, tokens, heads, strides):
+    return {start + b * strides[0] + n * strides[1] + h * strides[2] + c
+            for b in range(batch) for n in range(tokens) for h in range(heads) for c in range(D)}
+
+
+# Small layouts at random: none that shares an element with the other is taken, and of two with the same strides each that is apart is.
+def test_random_layouts(driver):
+    import random
+    rng = random.Random(5)
+    calls, want = [], []
+    while len(calls) < 4000:
+        batch, tokens, heads = [rng.choice([1, 1, 2, 3]) for _ in range(3)]
+        order, strides, reach = rng.sample(range(3), 3), [0, 0, 0], D
+        for i in order:
+            strides[i] = reach * rng.choice([1, 1, 2, 3]) + rng.choice([0, 0, 1, D])
+            reach = strides[i] * (batch, tokens, heads)[i]
+        k = rng.randrange(0, reach + D) if rng.random() < 0.5 else rng.choice(strides)
+        heads_k = rng.choice([heads, heads, 1, 2])
+        other = [s * rng.choice([1, 1, 1, 2]) for s in strides] if rng.random() < 0.2 else strides
+        apart = not _places(0, batch, tokens, heads, strides) & _places(k, batch, tokens, heads_k, other)
+        own = _places(k, batch, tokens, heads_k, other)
+        if len(own) < batch * tokens * heads_k * D:
+            continue
+        calls.append((GRID, D, DIMS, batch, tokens, [(A, A, heads, strides, strides), (A + 2 * k, A + 2 * k, heads_k, other, other)]))
+        want.append((apart, other == strides))
+    taken = 0
+    for call, (apart, same), status in zip(calls, want, _statuses(driver, calls)):
+        if not apart:
+            assert status == EINVAL, call
+        elif same:
+            assert status == OK, call
+            taken += 1
+    assert taken > 500
