@@ -289,6 +289,7 @@ __global__ __launch_bounds__(64 * grad_waves(WPR), (grad_per_cu<NV>())) void nor
         next_x[v] = take(x + p.col, p.here && row < end);
         next_d[v] = take(dy + p.col, p.here && row < end);
       }
+    next_mean = next_rstd = 0.f;
     if (row < end) next_mean = a.mean[row], next_rstd = a.rstd[row];
   };
   fetch(first + slot);
@@ -305,10 +306,16 @@ __global__ __launch_bounds__(64 * grad_waves(WPR), (grad_per_cu<NV>())) void nor
         const f32x8 x = Eight<X>::wide(next_x[v]), d = Eight<X>::wide(next_d[v]);
         f32x8 w = a.w0;
         if (a.weight) w += Eight<P>::wide(weight[v]);
-        const int skip = v * STEP + STEP <= a.cols ? 0 : piece_at(v * STEP + col0, a.cols).skip;
+        int skip = 0;
+        float r = rstd;
+        if (v * STEP + STEP > a.cols) {
+          const Piece p = piece_at(v * STEP + col0, a.cols);
+          skip = p.skip;
+          if (!p.here) r = 0.f;   // h is 0 where there is no piece: -mean * rstd may be infinite, and 0 times that is NaN
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          h[v][i] = (x[i] - mean) * rstd;
+          h[v][i] = (x[i] - mean) * r;
           g[v][i] = d[i] * w[i];   // 0 where there is no piece
           dw[v][i] = fmaf(d[i], h[v][i], dw[v][i]);
           db[v][i] += d[i];
@@ -379,7 +386,7 @@ __global__ __launch_bounds__(1024) void norm_grad_long_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float h = (f[i] - mean) * rstd;
-          if (pass == 0) sum_g += g[i], sum_gh = fmaf(g[i], h, sum_gh);   // g is 0 past the end
+          if (pass == 0) sum_g += g[i], sum_gh = fmaf(g[i], i < n ? h : 0.f, sum_gh);   // g is 0 past the end, -mean * rstd may be infinite
           else d[i] = rstd * (g[i] - sum_g - h * sum_gh);
         }
         if (pass == 1) store_eight((X*)a.dx + row * a.x_stride + col, d, n);
