@@ -361,7 +361,11 @@ def _norm_config(what, x, y, weight, bias, group_rows, weight_offset, eps):
             if p is weight and bias is not None and (stride != param_stride or p.dtype != bias.dtype):
                 _refuse(what, "weight and bias differ in stride or type")
             param_stride, param_type = stride, _type(p, what)
-    y_stride = _matrix(y, what, rows, cols if y_type != JENGA_E4M3 else padded_columns(cols))
+    if y_type == JENGA_E4M3:
+        y_stride = padded_columns(cols)
+        _whole(y, what, (rows, y_stride), "e4m3")
+    else:
+        y_stride = _matrix(y, what, rows, cols)
     return _pack(what, _NORM, rows, group_rows, x_stride, y_stride, param_stride, cols, x_type, y_type, param_type, eps, weight_offset)
 
 
