@@ -355,7 +355,7 @@ def _norm_config(what, x, y, weight, bias, group_rows, weight_offset, eps):
         if p is not None:
             shape, stride = p.shape, p.stride()
             groups = -(-rows // group_rows)
-            if shape[-1] != cols or stride[-1] != 1 and cols != 1 or len(shape) > 2 or (rows and (shape[0] if len(shape) == 2 else 1) != groups):
+            if not 1 <= len(shape) <= 2 or shape[-1] != cols or stride[-1] != 1 and cols != 1 or (rows and (shape[0] if len(shape) == 2 else 1) != groups):
                 _refuse(what, "weight or bias of shape %s" % (tuple(shape),))
             stride = stride[0] if groups > 1 else cols
             if p is weight and bias is not None and (stride != param_stride or p.dtype != bias.dtype):

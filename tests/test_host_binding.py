@@ -24,3 +24,12 @@ def test_rows_of_8_bits_lie_next_to_each_other():
         with pytest.raises(J.JengaError) as e:
             J.jenga_layer_norm(torch.zeros(2, 100), y, y_scale=torch.zeros(2, 4, dtype=torch.uint8))
         assert e.value.status == -1
+
+
+@pytest.mark.parametrize("shape", [(), (1, 1, 64)])
+def test_weights_that_are_no_rows_are_refused(shape):
+    x, y = torch.zeros(4, 64), torch.zeros(4, 64)
+    for kw in (dict(weight=torch.zeros(shape)), dict(bias=torch.zeros(shape))):
+        with pytest.raises(J.JengaError) as e:
+            J.jenga_layer_norm(x, y, **kw)
+        assert e.value.status == -1
