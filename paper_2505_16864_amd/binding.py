@@ -228,20 +228,21 @@ def jenga_stage_switch(x_t, eps_t, eps_tilde, x_out, channels, in_shape, out_sha
 
 
 # The calls around the attention take torch tensors and read sizes, strides and types from them.  What the C ABI cannot see is
-# checked here: values next to each other in the last dimension, all tensors on the device that is current.  Small calls cost little
-# more than this code and a launch, so it is written without detours.
+# checked here: values next to each other in the last dimension, all tensors on the device that is current.  They go to torch's current
+# stream of that device, where its own work on the tensors goes, unless `stream` names another (0: the null stream, which is
+# what None means to the calls above).  Small calls cost little more than this code and a launch, so it is written without detours.
 
 _EINVAL = -1
 _TYPES = {}            # torch's element types to jenga_type, filled by the first call that needs them
 _DTYPE = {}            # and by name
-_current_device = None
+_current_device = _current_stream = None
 _MATMUL, _NORM, _TENSOR = struct.Struct("=2q4i"), struct.Struct("=5q4i2f"), struct.Struct("=2Q6q2i")   # as the structures above
 
 
 def _use_torch():
     import torch
-    global _current_device
-    _current_device = torch._C._cuda_getDevice
+    global _current_device, _current_stream
+    _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _DTYPE.update(f32=torch.float32, i32=torch.int32, u8=torch.uint8, bf16=torch.bfloat16, e4m3=torch.float8_e4m3fn)
     _TYPES.update({torch.bfloat16: JENGA_BF16, torch.float16: JENGA_F16, torch.float32: JENGA_F32, torch.float8_e4m3fn: JENGA_E4M3,
                    torch.uint8: JENGA_E4M3})
@@ -269,13 +270,15 @@ def _type(t, what):
     return code
 
 
-def _on_device(what, tensors):
+def _on_device(what, tensors, stream):
+    """Refuses tensors that are not on the current device; returns the stream to go to."""
     device = tensors[0].get_device()
     for t in tensors:
         if t is not None and (t.get_device() != device or device < 0):
             _refuse(what, "tensors are not all on one GPU")
     if device != _current_device():
         _refuse(what, "tensors are not on the current device")
+    return _current_stream(device) if stream is None else stream
 
 
 def _matrix(t, what, rows=None, cols=None):
@@ -317,7 +320,7 @@ def jenga_quantize(x, q, scale, block_rows=1, stream=None):
         _refuse(what, "blocks of %s rows" % block_rows)
     _whole(q, what, (rows, padded_columns(cols)), "e4m3")
     _whole(scale, what, (-(-rows // block_rows), scale_columns(cols)), "u8")
-    _on_device(what, (x, q, scale))
+    stream = _on_device(what, (x, q, scale), stream)
     if cols > 0x7FFFFFFF:
         _refuse(what, "%d columns" % cols)
     if rows:
@@ -338,7 +341,7 @@ def jenga_matmul(a, a_scale, b, b_scale, out, bias=None, stream=None):
     _whole(b_scale, what, (-(-n // 128), scales), "u8")
     if bias is not None:
         _whole(bias, what, (n,), "f32")
-    _on_device(what, (a, a_scale, b, b_scale, out, bias))
+    stream = _on_device(what, (a, a_scale, b, b_scale, out, bias), stream)
     if m:
         _check(_lib.jenga_matmul(_pack(what, _MATMUL, m, stride, n, k, kind, 0), a.data_ptr(), a_scale.data_ptr(),
                                  b.data_ptr(), b_scale.data_ptr(), None if bias is None else bias.data_ptr(), out.data_ptr(), stream), what)
@@ -382,7 +385,7 @@ def jenga_layer_norm(x, y, weight=None, bias=None, y_scale=None, mean=None, rstd
         _whole(mean, what, (rows,), "f32")
     if rstd is not None:
         _whole(rstd, what, (rows,), "f32")
-    _on_device(what, (x, y, weight, bias, y_scale, mean, rstd))
+    stream = _on_device(what, (x, y, weight, bias, y_scale, mean, rstd), stream)
     if rows:
         _check(_lib.jenga_layer_norm(cfg, x.data_ptr(), None if weight is None else weight.data_ptr(),
                                      None if bias is None else bias.data_ptr(), y.data_ptr(),
@@ -416,7 +419,7 @@ def jenga_layer_norm_grad(x, dy, dx, weight, mean, rstd, dweight=None, dbias=Non
             if t.numel() != groups * cols:
                 _refuse(what, "gradients of %d groups" % groups)
             _whole(t, what, t.shape, "f32")
-    _on_device(what, (x, dy, dx, weight, mean, rstd, dweight, dbias, workspace))
+    stream = _on_device(what, (x, dy, dx, weight, mean, rstd, dweight, dbias, workspace), stream)
     if rows:
         _check(_lib.jenga_layer_norm_grad(cfg, x.data_ptr(), dy.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(),
                                           dx.data_ptr(), _ptr(dweight), _ptr(dbias), _ptr(workspace),
@@ -471,7 +474,7 @@ def jenga_rotary(cfg, table, q, q_out, k=None, k_out=None, cells=None, plan=None
     _rotary_table(cfg, table, what)
     if cells is not None:
         _whole(cells, what, (batch, tokens, 3), "i32")
-    _on_device(what, (q, q_out, k, k_out, table, cells))
+    stream = _on_device(what, (q, q_out, k, k_out, table, cells), stream)
     if batch and tokens:
         if cfg.type != kind:
             cfg = jenga_rotary_config.from_buffer_copy(cfg)
@@ -495,7 +498,7 @@ def jenga_forward_rotary(plan, cfg, table, q_thw, k_thw, v_thw, q_curve, k_curve
                 (tokens > 1 and s[1] != stride) or (batch > 1 and s[0] != stride * tokens):
             _refuse(what, "shape %s, strides %s, type %s" % (tuple(t.shape), s, t.dtype))
     _rotary_table(cfg, table, what)
-    _on_device(what, (table, q_thw, k_thw, v_thw))
+    stream = _on_device(what, (table, q_thw, k_thw, v_thw), stream)
     _check(_lib.jenga_forward_rotary(plan, ctypes.byref(cfg), _ptr(table), _ptr(q_thw), _ptr(k_thw), _ptr(v_thw), stride, _ptr(q_curve),
                                      _ptr(k_curve), _ptr(v_curve), _ptr(sel_count), _ptr(sel_index), _ptr(mask),
                                      _ptr(select_workspace), select_workspace_bytes, _ptr(out_curve), _ptr(lse),
