@@ -67,6 +67,31 @@ StageTiles stage_switch_tiles(long long channels, int T_in, int H_in, int W_in, 
   return s;
 }
 
+// Figures in us, with weights that no cache holds but where 256 x 256 is compared.
+MatmulTiles matmul_tiles(int64_t m, int64_t n, bool float32) {
+  auto tiles = [&](int bm, int bn) { return (m + bm - 1) / bm * ((n + bn - 1) / bn); };
+  auto rounds = [](int64_t t, int at_once) { return (t + at_once - 1) / at_once; };
+  // Up to 16 rows without tiles, up to 32 where their second reading by each 16 columns is short.  Rows -> 64 x 128: 16 x 5120 x 5120
+  // 12.9 -> 20.8; 16 x 15360 24.0 -> 23.3; 20 x 1536 x 1536 6.8 -> 8.0; 20 x 5120 x 5120 16.4 -> 21.1; 32 19.1 -> 22.4; 32 x 9216 x 1536
+  // 11.7 -> 9.5; 48 x 5120 x 5120 (three times 16) 24.8 -> 23.7.
+  if (m <= 16) return {16, 0, 0, 0, 0};
+  if (m <= 32 && n <= 6144) return {32, 0, 0, 0, 0};
+  // Tiles of 256 x 256 read each row of either operand half as often as those of 128 x 128; a round of them (one a compute unit) takes 1.5 to
+  // 1.65 times as long as a round of the others (two a unit).  256 -> 128, by rounds of either: 1 and 1, 1500 x 5120 x 5120 55.5 -> 40.7; 1 and 2, 2048
+  // 57.5 -> 71.1, 3000 63.8 -> 78.2; 2 and 3, 4096 117.9 -> 112.0, 4864 121.5 -> 121.0, 4096 x 5120 x 1536 43.3 -> 38.6, 4500 x 4700 x 2048 62.8 ->
+  // 57.2; 3 and 5, 9000 x 4000 x 4096 150.2 -> 150.9, 7000 x 5000 x 5120 187.2 -> 191.6; 2 and 4, 5120 x 5120 x 5120 119.6 -> 146.7; 31 and 61,
+  // 33272 x 15360 2144 -> 2603.  (4 and 7, 11264 x 4608 x 1536 loses by it, 93.0 -> 89.6: a short k favours 128.)
+  if (!float32 && 1.55 * rounds(tiles(256, 256), 256) <= rounds(tiles(128, 128), 512)) return {0, 256, 256, 2, 1};
+  // No more tiles than units: one a unit, four LDS tiles deep, which is what hides the memory's latency then (two -> three -> four -> five ->
+  // six deep: 64 x 5120 x 5120 40.2 -> 29.5 -> 25.4 -> 25.9 -> 26.2).  64 x 128, or 128 x 128 where the former are more than units.  64 x 128
+  // two deep, two a unit -> four deep -> 128 x 128 four deep: 256 x 5120 x 5120 (160 and 80) 36.9 -> 23.5 -> 31.4; 400 (280 and 160) 36.9 ->
+  // 37.6 -> 29.1; 900 x 4096 x 4096 (480 and 256) 31.4 -> 32.0 -> 24.1; float32 200 x 5120 x 5120 41.9 -> 31.2 -> 41.6, 900 x 4096 x 4096
+  // 41.7 -> 50.9 -> 40.2.
+  if (tiles(64, 128) <= 256) return {0, 64, 128, 4, 1};
+  if (tiles(128, 128) <= 256) return {0, 128, 128, 4, 1};
+  return {0, 128, 128, 2, 2};
+}
+
 // ---- arguments of the calls around the attention
 
 namespace {

@@ -190,6 +190,14 @@ struct GridCells {
   }
 };
 
+// Which kernel multiplies m rows by n columns; float32: the one for float32 results, which has no tiles of 256.
+struct MatmulTiles {
+  int rows;                 // 16 or 32: rows without tiles, up to so many; else 0
+  int bm, bn, stages;       // results of a tile, LDS tiles
+  int per_cu;               // workgroups on a compute unit
+};
+MatmulTiles matmul_tiles(int64_t m, int64_t n, bool float32);
+
 // Checks of arguments (jenga_host.cpp), all of a call's that need no device.  They return a jenga_status.
 int norm_args_ok(const jenga_norm_config* c, const void* x, const void* weight, const void* bias, const void* y, const uint8_t* y_scale,
                  const float* mean, const float* rstd);

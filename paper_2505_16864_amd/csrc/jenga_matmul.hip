@@ -487,27 +487,14 @@ int run_rows(const MatmulArgs& g, hipStream_t st) {
 
 template <typename O, bool EXACT>
 int run_matmul(const MatmulArgs& g, hipStream_t st) {
-  auto tiles = [&](int bm, int bn) { return (g.m + bm - 1) / bm * ((g.n + bn - 1) / bn); };
-  auto rounds = [&](int64_t n, int at_once) { return (n + at_once - 1) / at_once; };
-  // Figures in us, with weights that no cache holds but where 256 x 256 is compared.
-  // Up to 16 rows without tiles, up to 32 where their second reading by each 16 columns is short.  Rows -> 64 x 128: 16 x 5120 x 5120
-  // 12.9 -> 20.8; 16 x 15360 24.0 -> 23.3; 20 x 1536 x 1536 6.8 -> 8.0; 20 x 5120 x 5120 16.4 -> 21.1; 32 19.1 -> 22.4; 32 x 9216 x 1536
-  // 11.7 -> 9.5; 48 x 5120 x 5120 (three times 16) 24.8 -> 23.7.
-  if (g.m <= 16) return run_rows<O, EXACT, 1>(g, st);
-  if (g.m <= 32 && g.n <= 6144) return run_rows<O, EXACT, 2>(g, st);
-  // Tiles of 256 x 256 read each row of either operand half as often as those of 128 x 128, a round of them (one a compute unit) takes 1.45
-  // times as long as a round of the others (two a unit).  256 -> 128: 1500 x 5120 x 5120 (120 tiles, one round each) 55.5 -> 40.7; 2048 (1
-  // and 2 rounds) 58.2 -> 71.5; 3000 (1 and 2) 65.7 -> 79.1; 4096 (2 and 3) 118.1 -> 113.5; 33272 x 15360 (31 and 61) 2144 -> 2603.
+  const jenga::MatmulTiles t = jenga::matmul_tiles(g.m, g.n, EXACT);
+  if (t.rows == 16) return run_rows<O, EXACT, 1>(g, st);
+  if (t.rows == 32) return run_rows<O, EXACT, 2>(g, st);
   if constexpr (!EXACT)
-    if (1.45 * rounds(tiles(256, 256), 256) <= rounds(tiles(128, 128), 512)) return run_tiles<O, EXACT, 256, 256, 2>(g, 1, st);
-  // No more tiles than units: one a unit, four LDS tiles deep, which is what hides the memory's latency then (two -> three -> four -> five ->
-  // six deep: 64 x 5120 x 5120 40.2 -> 29.5 -> 25.4 -> 25.9 -> 26.2).  64 x 128, or 128 x 128 where the former are more than units.  64 x 128
-  // two deep, two a unit -> four deep -> 128 x 128 four deep: 256 x 5120 x 5120 (160 and 80) 36.9 -> 23.5 -> 31.4; 400 (280 and 160) 36.9 ->
-  // 37.6 -> 29.1; 900 x 4096 x 4096 (480 and 256) 31.4 -> 32.0 -> 24.1; float32 200 x 5120 x 5120 41.9 -> 31.2 -> 41.6, 900 x 4096 x 4096
-  // 41.7 -> 50.9 -> 40.2.
-  if (tiles(64, 128) <= 256) return run_tiles<O, EXACT, 64, 128, 4>(g, 1, st);
-  if (tiles(128, 128) <= 256) return run_tiles<O, EXACT, 128, 128, 4>(g, 1, st);
-  return run_tiles<O, EXACT, 128, 128, 2>(g, 2, st);
+    if (t.bm == 256) return run_tiles<O, EXACT, 256, 256, 2>(g, t.per_cu, st);
+  if (t.bm == 64) return run_tiles<O, EXACT, 64, 128, 4>(g, t.per_cu, st);
+  if (t.stages == 4) return run_tiles<O, EXACT, 128, 128, 4>(g, t.per_cu, st);
+  return run_tiles<O, EXACT, 128, 128, 2>(g, t.per_cu, st);
 }
 
 template <typename X>
