@@ -37,3 +37,20 @@ def tiles(tmp_path_factory):
 def test_large_tiles_where_they_were_faster(tiles, m, n, bm):
     assert tiles([(m, n, "bf16")])[0][1] == bm
     assert tiles([(m, n, "f32")])[0][1] == 128
+
+
+# The sizes that the GPU tests multiply reach every kernel that the rule can name, several tiles a workgroup among them.
+def test_tested_sizes_reach_every_kernel(tiles):
+    import random
+    from matmul_sizes import CASES, SIZES
+    at_once = {}
+    for (kernel, m, n, _, out), got in zip(CASES, tiles([(m, n, out) for _, m, n, _, out in CASES])):
+        assert got[:4] == kernel, (m, n, out)
+        if kernel[1]:
+            at_once.setdefault((kernel, out), []).append(-(-m // kernel[1]) * -(-n // kernel[2]) / (256 * got[4]))
+    for key, rounds in at_once.items():
+        assert min(rounds) <= 1 and (key[0][3] == 4 or max(rounds) > 1.5), key
+    rng = random.Random(1)
+    drawn = [(int(2 ** rng.uniform(0, 16)), int(2 ** rng.uniform(0, 15)), rng.choice(["bf16", "f32"])) for _ in range(20000)]
+    for size, got in zip(drawn, tiles(drawn)):
+        assert got[:4] in SIZES and (got[1] != 256 or size[2] != "f32"), size
