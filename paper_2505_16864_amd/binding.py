@@ -230,7 +230,8 @@ def jenga_stage_switch(x_t, eps_t, eps_tilde, x_out, channels, in_shape, out_sha
 # The calls around the attention take torch tensors and read sizes, strides and types from them.  What the C ABI cannot see is
 # checked here: values next to each other in the last dimension, all tensors on the device that is current.  They go to torch's current
 # stream of that device, where its own work on the tensors goes, unless `stream` names another (0: the null stream, which is
-# what None means to the calls above).  Small calls cost little more than this code and a launch, so it is written without detours.
+# what None means to the calls above).  No gradient is recorded: tensors that require one are taken like others.  Small calls cost
+# little more than this code and a launch, so it is written without detours.
 
 _EINVAL = -1
 _TYPES = {}            # torch's element types to jenga_type, filled by the first call that needs them

