@@ -6,7 +6,7 @@ spread, h = 0 and rstd = 1 / sqrt(eps) = 2^10 for eps = 2^-20.  So dx = rstd (g 
 import pytest
 import torch
 
-from operator_util import TYPES, U32, check, half_step, randn
+from operator_util import TYPES, U32, check, half_step, held_values, quantize, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +56,31 @@ def test_statistics_far_apart(rows, cols):
     check(dx, want, half_step(torch.float32) * want.abs() + slack * 1.01, "dx")
     assert not dw.any()
     check(db, g.sum(0), U32 * (rows + 8) * g.abs().sum(0), "dbias")
+
+
+# 8-bit results with a scale and a shift for each of several groups, one of them short, rows that lie apart, an odd number of columns too:
+# the bits that quantising the float32 result gives, but where that is a rounding's width off a border.
+@pytest.mark.parametrize("rows,cols,group_rows", [(10, 96, 4), (7, 1000, 1), (33, 1536, 12), (5, 130, 2), (9, 2048, 5), (3, 8200, 2)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_eight_bit_results_of_groups(rows, cols, group_rows, dtype):
+    import paper_2505_16864_amd as J
+    groups = -(-rows // group_rows)
+    room = randn(rows + cols, rows, cols + 7).to(TYPES[dtype]).cuda()
+    x = room[:, 3:3 + cols]
+    params = (0.4 * randn(3, groups, 2 * cols + 1)).to(TYPES[dtype]).cuda()
+    w, b = params[:, :cols], params[:, cols + 1:]
+    q = torch.full((rows, J.padded_columns(cols)), 99, dtype=torch.uint8, device="cuda:0")
+    s = torch.full((rows, J.scale_columns(cols)), 99, dtype=torch.uint8, device="cuda:0")
+    J.jenga_layer_norm(x, q, w, b, y_scale=s, group_rows=group_rows, weight_offset=1.0)
+    y = torch.empty((rows, cols), device="cuda:0")
+    J.jenga_layer_norm(x.float(), y, w.float(), b.float(), group_rows=group_rows, weight_offset=1.0)
+    torch.cuda.synchronize()
+    want, want_scale = quantize(y.cpu().double(), 1)
+    got = held_values(q, s, 1)
+    assert not q[:, cols:].any()
+    # the same values in float32 in another order at most; a border's other side is a step of e4m3 away, 2^-3 of the value, twice that
+    # where the scale is on the other side too
+    blocks = -(-cols // 128)
+    unit = torch.ldexp(torch.ones(rows, blocks, dtype=torch.float64), want_scale[:, :blocks].int() - 127).repeat_interleave(128, 1)
+    assert bool(((got - want).abs() <= 2 * torch.maximum(2.0 ** -3 * want.abs(), 2.0 ** -9 * unit)).all())
+    assert float((got != want).double().mean()) <= 0.01

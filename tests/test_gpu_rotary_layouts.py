@@ -54,3 +54,22 @@ def test_refuses_a_shared_part(tokens):
     assert e.value.status == -1
     torch.cuda.synchronize()
     assert not room.any()
+
+
+# From one layout to another: tokens first to heads first, one head for all (stride 0), one sequence for all, K beside Q with fewer heads.
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("head_dim,dims", [(64, (16, 24, 24)), (10, (2, 4, 2))])
+@pytest.mark.parametrize("tokens", [1, 37])
+def test_from_one_layout_to_another(tokens, head_dim, dims, halves):
+    import paper_2505_16864_amd as J
+    cfg = J.make_rotary(*GRID, head_dim, dims, flags=J.JENGA_ROTARY_HALVES if halves else 0)
+    table = torch.empty(sum(n * d for n, d in zip(GRID, dims)))
+    J.jenga_rotary_table(cfg, table)
+    q, k = randn(1, 3, tokens, 1, head_dim).to(torch.bfloat16), randn(2, 1, tokens, 2, head_dim).to(torch.bfloat16)
+    q_out, k_out = [torch.full((3, heads, tokens, head_dim), 7.0, dtype=torch.bfloat16, device="cuda:0").transpose(1, 2) for heads in (5, 2)]
+    J.jenga_rotary(cfg, table.cuda(), q.cuda().expand(-1, -1, 5, -1), q_out, k.cuda().expand(3, -1, -1, -1), k_out)
+    torch.cuda.synchronize()
+    for got, x in ((q_out, q.double().expand(-1, -1, 5, -1)), (k_out, k.double().expand(3, -1, -1, -1))):
+        want = rotary(x, *GRID, dims, 10000.0, halves=halves)
+        top = x.abs().topk(2, dim=-1).values.sum(-1, keepdim=True)
+        check(got, want, half_step(torch.bfloat16) * want.abs() + 4 * U32 * top * 1.01)
