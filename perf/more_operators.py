@@ -266,13 +266,13 @@ def _own(state):
                 out += [p["dx"], p["dweight"]]
         return out
     if kind == "matmul":
-        J.jenga_quantize_mx4(state["x"], state["a"], state["a_scale"])
-        J.jenga_matmul_mx4(state["a"], state["a_scale"], state["w"], state["w_scale"], state["out"], state["bias"])
+        J.jenga_quantize_mx(state["x"], state["a"], state["a_scale"])
+        J.jenga_matmul_mx(state["a"], state["a_scale"], state["w"], state["w_scale"], state["out"], state["bias"])
         return state["out"]
     if kind == "project":
         J.jenga_rms_norm(state["x"], state["a"], state["weight"], residual=state["residual"], total=state["total"],
                          y_scale=state["a_scale"], eps=EPS)
-        product = J.jenga_matmul_mx4 if case["bits"] == 4 else J.jenga_matmul
+        product = J.jenga_matmul_mx if case["bits"] == 4 else J.jenga_matmul
         product(state["a"], state["a_scale"], state["w"], state["w_scale"], state["out"], state["bias"])
         return [state["total"], state["out"]]
     J.jenga_dense_attn(state["q"], state["k"], state["v"], state["out"], state["q_start"], state["kv_start"], causal=case["causal"],
