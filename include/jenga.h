@@ -12,8 +12,9 @@
  *   jenga_stage_switch      resolution switch between stages      Eq. 4
  *
  * and what a transformer block has in front of that attention and behind it: layer norm and its gradient
- * (jenga_layer_norm), matrix products in 8-bit floating point (jenga_quantize, jenga_matmul), rotary positions
- * over time, height and width (jenga_rotary, jenga_forward_rotary).
+ * (jenga_layer_norm), the norm without a mean (jenga_rms_norm), matrix products in 8-bit and 4-bit floating point
+ * (jenga_quantize, jenga_matmul, jenga_quantize_mx, jenga_matmul_mx), rotary positions over time, height and width
+ * (jenga_rotary, jenga_forward_rotary), and attention to all keys for what is not carved (jenga_dense_attn).
  *
  * Conventions
  *   - All tensor arguments are DEVICE pointers unless a comment says "host".  The caller owns
@@ -280,8 +281,9 @@ int jenga_stage_switch(const float* x_t, const float* eps_t, const float* eps_ti
  * JENGA_EINVAL.  Calls with no rows return JENGA_OK and touch nothing.
  */
 
-/* Types of elements.  JENGA_E4M3: OCP 8-bit floating point, 4 exponent and 3 mantissa bits, no infinities. */
-typedef enum { JENGA_BF16 = 0, JENGA_F16 = 1, JENGA_F32 = 2, JENGA_E4M3 = 3 } jenga_type;
+/* Types of elements.  JENGA_E4M3: OCP 8-bit floating point, 4 exponent and 3 mantissa bits, no infinities.  JENGA_E2M1: OCP 4-bit
+ * floating point, 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (jenga_rms_norm's results only). */
+typedef enum { JENGA_BF16 = 0, JENGA_F16 = 1, JENGA_F32 = 2, JENGA_E4M3 = 3, JENGA_E2M1 = 4 } jenga_type;
 
 /*
  * 8-bit tensors.  A matrix of r rows and c columns is held as
@@ -331,6 +333,30 @@ int jenga_matmul(const jenga_matmul_config* cfg, const void* a, const uint8_t* a
                  const uint8_t* b_scale, const float* bias_or_null, void* out, void* stream);
 
 /*
+ * 4-bit tensors.  A matrix of r rows and c columns is held as
+ *   values  e2m1 [r][C / 2], C = c rounded up to a multiple of 128, two values a byte, the one of the even column in the low four
+ *           bits (sign, two bits of exponent, one of mantissa); the columns that fill up are 0.  16-byte aligned
+ *   scales  uint8 [r][C / 32], a byte e + 127 for the scale 2^e of each 32 columns of a row.  4-byte aligned
+ * and stands for values * 2^e.  e is the least whole number >= -127 with |x| <= 6 * 2^e for all x of the block (0 where they are
+ * all 0): nothing saturates, and the only rounding is the one to e2m1, to nearest, ties to the even one.  There is no NaN among
+ * the values: a block with an infinity or a NaN has the byte 255, which makes all of it NaN in a product.
+ */
+
+/*
+ * x -> 4-bit tensor.  x as in jenga_quantize, with its limits.
+ */
+int jenga_quantize_mx(const void* x, int64_t x_stride, int32_t x_type, int64_t rows, int32_t cols, void* q, uint8_t* scale,
+                      void* stream);
+
+/*
+ * Product of two 4-bit tensors, a [m][k] and b [n][k]:
+ *   out[i][j] = sum over blocks kb of 32 of 2^(ea[i][kb] + eb[j][kb]) * sum over k in kb of a[i][k] b[j][k] + bias[j]
+ * cfg, bias and out as in jenga_matmul.  Products are exact, sums float32 and rounded once to out's type.
+ */
+int jenga_matmul_mx(const jenga_matmul_config* cfg, const void* a, const uint8_t* a_scale, const void* b,
+                    const uint8_t* b_scale, const float* bias_or_null, void* out, void* stream);
+
+/*
  * Layer norm over the columns of each row.  Rows come in groups of group_rows consecutive ones (the last may be
  * short) that share a weight and a bias: all rows in one group are the ordinary affine norm, a group for each batch
  * entry with weight_offset 1 the modulation of a diffusion transformer, (1 + scale) and shift.
@@ -377,6 +403,56 @@ int jenga_layer_norm_grad(const jenga_norm_config* cfg, const void* x, const voi
 
 /* Bytes of its workspace (host only): (1024 + groups) * cols * 8. */
 int jenga_layer_norm_grad_workspace(const jenga_norm_config* cfg, uint64_t* bytes);
+
+/*
+ * Root-mean-square norm (no mean is taken off) over the columns of each row, or of each head of a row, with one weight for all of them, and
+ * the addition of a residual stream in front of it.  Tensors are [rows][heads][cols]; strides in elements, from row to row and from
+ * head to head: any >= 0, but no two elements of a result in one place.
+ */
+typedef struct {
+  int64_t rows;                 /* >= 0                                                             */
+  int64_t x_row, x_head;        /* strides of x                                                     */
+  int64_t add_row, add_head;    /* of residual (dtotal in the gradient); not looked at without it   */
+  int64_t sum_row, sum_head;    /* of total (dx in the gradient); not looked at without it          */
+  int64_t y_row, y_head;        /* of y (dy in the gradient); not looked at in 8 and 4 bits         */
+  int32_t heads, cols;          /* >= 1 (1 for results in 8 and 4 bits); 1 to 2^17                  */
+  int32_t x_type;               /* JENGA_BF16, JENGA_F16 or JENGA_F32: of x, residual and total     */
+  int32_t y_type;               /* x_type, or in the forward pass JENGA_E4M3 or JENGA_E2M1          */
+  int32_t param_type;           /* of weight: x_type or JENGA_F32                                   */
+  float eps, weight_offset;     /* finite, eps >= 0                                                 */
+  int32_t reserved;             /* 0                                                                */
+} jenga_rms_config;
+
+/*
+ *   total = x + residual, rounded to x_type (x itself without a residual)
+ *   r = 1 / sqrt(mean(total^2) + eps)   y = total r (weight_offset + weight)
+ *   weight : param_type [cols], or NULL for zeros
+ *   total  : or NULL; may be x or residual itself (same address and strides)
+ *   y      : may be x or residual itself.  JENGA_E4M3: an 8-bit tensor with blocks of 1 x 128, JENGA_E2M1: a 4-bit one; scales in
+ *            y_scale (else NULL)
+ *   rstd   : float32 [rows][heads], r for the gradient, or NULL
+ * Sums are float32 (squares above 3.4e38 are infinite), y is rounded once.  JENGA_EUNSUPPORTED: 2^31 heads of rows and more where heads > 1.
+ */
+int jenga_rms_norm(const jenga_rms_config* cfg, const void* x, const void* residual_or_null, const void* weight_or_null,
+                   void* total_or_null, void* y, uint8_t* y_scale_or_null, float* rstd_or_null, void* stream);
+
+/*
+ * Its gradient with respect to total (the same for x and residual), from dy and from what comes to total by other ways:
+ *   h = total rstd   g = dy (weight_offset + weight)   dx = rstd (g - h mean(g h)) + dtotal   dweight = sum over rows and heads of dy h
+ *   x       : total of the forward pass
+ *   dtotal  : x_type, or NULL
+ *   dx      : x_type; may be dtotal itself
+ *   dweight : float32 [cols], fully overwritten, or NULL
+ *   workspace : jenga_rms_norm_grad_workspace bytes, 256-byte aligned, contents undefined after; NULL without dweight.  Calls that may run
+ *             at the same time need one each
+ * Sums are float32 and in an order that depends on the sizes alone.
+ */
+int jenga_rms_norm_grad(const jenga_rms_config* cfg, const void* x, const void* dy, const void* weight_or_null, const float* rstd,
+                        const void* dtotal_or_null, void* dx, float* dweight_or_null, void* workspace, size_t workspace_bytes,
+                        void* stream);
+
+/* Bytes of its workspace (host only): 1024 * cols * 4. */
+int jenga_rms_norm_grad_workspace(const jenga_rms_config* cfg, uint64_t* bytes);
 
 /*
  * Rotary positions over the axes of a T x H x W grid.  The first dim[0] channels of a head turn with the token's
@@ -446,6 +522,50 @@ int jenga_forward_rotary(const jenga_plan* plan, const jenga_rotary_config* rota
                          void* v_curve, int32_t* sel_count, int32_t* sel_index, uint8_t* mask_or_null,
                          void* select_workspace, size_t select_workspace_bytes, void* out_curve, float* lse_or_null,
                          void* attn_workspace, size_t attn_workspace_bytes, void* out_thw, void* stream);
+
+/*
+ * Softmax attention of packed sequences to all of their keys: text tokens, cross attention to text, prompts, layers that are not
+ * carved, and one new token for each of many cached sequences.
+ */
+enum { JENGA_DENSE_CAUSAL = 1u };
+typedef struct {
+  int64_t q_rows, kv_rows;      /* of q and out; of k and v; each 0 to 2^31 - 1                     */
+  int64_t q_row, q_head;        /* strides in elements, >= 0; no two elements of out in one place */
+  int64_t k_row, k_head, v_row, v_head;
+  int64_t out_row, out_head;
+  int32_t sequences;            /* >= 0                                                             */
+  int32_t heads, kv_heads;      /* >= 1; heads a multiple of kv_heads: head h attends to h / (heads / kv_heads) */
+  int32_t head_dim;             /* 64 or 128                                                        */
+  int32_t type;                 /* JENGA_BF16 or JENGA_F16                                          */
+  uint32_t flags;               /* JENGA_DENSE_*                                                    */
+  float scale;                  /* of the logits, finite and > 0: 1 / sqrt(head_dim) as a rule      */
+  int32_t reserved;             /* 0                                                                */
+} jenga_dense_config;
+
+/*
+ *   out_i = sum over j of p_ij v_j / sum over j of p_ij,   p_ij = exp(scale q_i k_j)
+ * for the rows i and keys j of each sequence and every head; JENGA_DENSE_CAUSAL: keys j <= i + n_kv - n_q only, so that the last
+ * row of a sequence sees all its keys.  Rows that see no key are 0.
+ *   q, out   : [q_rows][heads][head_dim]; rows of sequence s are q_start[s] to q_start[s + 1] - 1.  Rows in front of the first and behind
+ *              the last sequence are left as they are.  out may be q itself (same address and strides)
+ *   k, v     : [kv_rows][kv_heads][head_dim]
+ *   q_start  : int32 [sequences + 1], on the device, ascending
+ *   kv_start : int32 [sequences + 1], likewise.  With kv_len (int32 [sequences], on the device) keys of sequence s are
+ *              kv_start[s] to kv_start[s] + kv_len[s] - 1 (a cache with room behind each sequence; the last start is not looked at
+ *              then, and keys may be shared), else up to kv_start[s + 1] - 1
+ *   workspace: jenga_dense_attn_workspace bytes, 256-byte aligned, contents undefined after.  Calls that may run at the same time need
+ *              one each
+ * Starts and lengths are cut to what is there on the device, so that no malformed number causes an access out of range.  What rows do not
+ * see does not touch them, whatever it holds.  Products of 16 bits, sums and softmax float32; the probabilities are rounded to
+ * 16 bits, the sum that divides them is not.  Results do not depend on the order of execution: the same call gives the same bits.
+ * JENGA_EUNSUPPORTED: another head_dim, more than 2^16 sequences, 2^12 heads or 2^30 rows with their heads, row strides above 2^23.
+ */
+int jenga_dense_attn(const jenga_dense_config* cfg, const void* q, const void* k, const void* v, const int32_t* q_start,
+                     const int32_t* kv_start, const int32_t* kv_len_or_null, void* out, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+/* Bytes of its workspace (host only); strides are not looked at. */
+int jenga_dense_attn_workspace(const jenga_dense_config* cfg, uint64_t* bytes);
 
 /* Static, NUL-terminated description of a status code. */
 const char* jenga_strerror(int status);

@@ -15,7 +15,8 @@ JENGA_FLAG_CONDITION = 2
 JENGA_FLAG_CURVE = 4
 JENGA_FLAG_PACED_WALK = 8
 
-JENGA_BF16, JENGA_F16, JENGA_F32, JENGA_E4M3 = range(4)
+JENGA_BF16, JENGA_F16, JENGA_F32, JENGA_E4M3, JENGA_E2M1 = range(5)
+JENGA_DENSE_CAUSAL = 1
 JENGA_ROTARY_HALVES = 1
 JENGA_ROTARY_INVERSE = 2
 
@@ -25,6 +26,8 @@ EXPORTS = ["jenga_plan_create", "jenga_plan_destroy", "jenga_plan_info", "jenga_
            "jenga_block_sparse_attn", "jenga_pack_kv",
            "jenga_block_sparse_attn_packed", "jenga_unpermute", "jenga_forward", "jenga_stage_switch",
            "jenga_quantize", "jenga_matmul", "jenga_layer_norm", "jenga_layer_norm_grad", "jenga_layer_norm_grad_workspace",
+           "jenga_quantize_mx", "jenga_matmul_mx", "jenga_rms_norm", "jenga_rms_norm_grad", "jenga_rms_norm_grad_workspace",
+           "jenga_dense_attn", "jenga_dense_attn_workspace",
            "jenga_rotary_table", "jenga_rotary", "jenga_forward_rotary", "jenga_strerror"]
 
 
@@ -50,6 +53,19 @@ class jenga_norm_config(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("group_rows", ctypes.c_int64), ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
                 ("param_stride", ctypes.c_int64), ("cols", ctypes.c_int32), ("x_type", ctypes.c_int32), ("y_type", ctypes.c_int32),
                 ("param_type", ctypes.c_int32), ("eps", ctypes.c_float), ("weight_offset", ctypes.c_float)]
+
+
+class jenga_rms_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "x_row", "x_head", "add_row", "add_head", "sum_row", "sum_head", "y_row", "y_head")] + \
+               [(n, ctypes.c_int32) for n in ("heads", "cols", "x_type", "y_type", "param_type")] + \
+               [("eps", ctypes.c_float), ("weight_offset", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class jenga_dense_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("q_rows", "kv_rows", "q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "out_row",
+                                              "out_head")] + \
+               [(n, ctypes.c_int32) for n in ("sequences", "heads", "kv_heads", "head_dim", "type")] + \
+               [("flags", ctypes.c_uint32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
 
 
 class jenga_rotary_config(ctypes.Structure):
@@ -100,6 +116,13 @@ def _load():
     lib.jenga_layer_norm.argtypes = [vp] * 9
     lib.jenga_layer_norm_grad.argtypes = [vp] * 10 + [size, vp]
     lib.jenga_layer_norm_grad_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
+    lib.jenga_quantize_mx.argtypes = [vp, i64, i32, i64, i32, vp, vp, vp]
+    lib.jenga_matmul_mx.argtypes = [vp] * 8
+    lib.jenga_rms_norm.argtypes = [vp] * 9
+    lib.jenga_rms_norm_grad.argtypes = [vp] * 9 + [size, vp]
+    lib.jenga_rms_norm_grad_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
+    lib.jenga_dense_attn.argtypes = [vp] * 9 + [size, vp]
+    lib.jenga_dense_attn_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
     lib.jenga_rotary_table.argtypes = [ctypes.POINTER(jenga_rotary_config), vp]
     lib.jenga_rotary.argtypes = [vp] * 5 + [i32, i64, i64, vp]
     lib.jenga_forward_rotary.argtypes = [vp, ctypes.POINTER(jenga_rotary_config)] + [vp] * 4 + [i64] + [vp] * 7 + [size, vp, vp, vp,
@@ -238,6 +261,7 @@ _TYPES = {}            # torch's element types to jenga_type, filled by the firs
 _DTYPE = {}            # and by name
 _current_device = _current_stream = None
 _MATMUL, _NORM, _TENSOR = struct.Struct("=2q4i"), struct.Struct("=5q4i2f"), struct.Struct("=2Q6q2i")   # as the structures above
+_RMS, _DENSE = struct.Struct("=9q5i2fi"), struct.Struct("=10q5iIfi")
 
 
 def _use_torch():
@@ -425,6 +449,177 @@ def jenga_layer_norm_grad(x, dy, dx, weight, mean, rstd, dweight=None, dbias=Non
         _check(_lib.jenga_layer_norm_grad(cfg, x.data_ptr(), dy.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(),
                                           dx.data_ptr(), _ptr(dweight), _ptr(dbias), _ptr(workspace),
                                           0 if workspace is None else workspace.numel() * workspace.element_size(), stream), what)
+
+
+def jenga_quantize_mx(x, q, scale, stream=None):
+    """x [rows, cols] -> 4-bit tensor: q uint8 [rows, padded_columns(cols) / 2], scale uint8 [rows, padded_columns(cols) / 32]."""
+    what = "jenga_quantize_mx"
+    stride, kind = _matrix(x, what), _type(x, what)
+    rows, cols = x.shape
+    padded = padded_columns(cols)
+    _whole(q, what, (rows, padded // 2), "u8")
+    _whole(scale, what, (rows, padded // 32), "u8")
+    stream = _on_device(what, (x, q, scale), stream)
+    if cols > 0x7FFFFFFF:
+        _refuse(what, "%d columns" % cols)
+    if rows:
+        _check(_lib.jenga_quantize_mx(x.data_ptr(), stride, kind, rows, cols, q.data_ptr(), scale.data_ptr(), stream), what)
+
+
+def jenga_matmul_mx(a, a_scale, b, b_scale, out, bias=None, stream=None):
+    """out [m, n] = a b^T + bias for 4-bit tensors, a uint8 [m, k / 2] and b uint8 [n, k / 2] with a scale for each 32 values; bias
+    float32 [n]."""
+    what = "jenga_matmul_mx"
+    if len(a.shape) != 2 or len(b.shape) != 2:
+        _refuse(what, "shapes %s, %s" % (tuple(a.shape), tuple(b.shape)))
+    (m, half), n, kind = a.shape, b.shape[0], _type(out, what)
+    stride = _matrix(out, what, m, n)
+    _whole(a, what, (m, half), "u8")
+    _whole(b, what, (n, half), "u8")
+    _whole(a_scale, what, (m, half // 16), "u8")
+    _whole(b_scale, what, (n, half // 16), "u8")
+    if bias is not None:
+        _whole(bias, what, (n,), "f32")
+    stream = _on_device(what, (a, a_scale, b, b_scale, out, bias), stream)
+    if m:
+        _check(_lib.jenga_matmul_mx(_pack(what, _MATMUL, m, stride, n, 2 * half, kind, 0), a.data_ptr(), a_scale.data_ptr(),
+                                    b.data_ptr(), b_scale.data_ptr(), None if bias is None else bias.data_ptr(), out.data_ptr(), stream), what)
+
+
+def _heads(t, what, shape=None, dtype=None):
+    """Row and head stride of [rows, cols] or [rows, heads, cols]; along an axis of one any stride will do."""
+    have = t.shape
+    if len(have) not in (2, 3) if shape is None else (have != shape or t.dtype != dtype):
+        _refuse(what, "shape %s, type %s" % (tuple(have), t.dtype))
+    stride = t.stride()
+    if stride[-1] != 1 and have[-1] != 1:
+        _refuse(what, "values of a row are not next to each other")
+    return stride[0] if have[0] > 1 else 0, stride[1] if len(have) == 3 and have[1] > 1 else 0
+
+
+def jenga_rms_norm(x, y, weight=None, residual=None, total=None, y_scale=None, rstd=None, weight_offset=0.0, eps=1e-6, stream=None):
+    """x, residual, total [rows, cols] or [rows, heads, cols] of one type, each with strides of its own; y the same, or of [rows, cols] an
+    8-bit (e4m3) or 4-bit (uint8) tensor with its scales in y_scale; weight [cols]; rstd float32 [rows] or [rows, heads].  total, or y,
+    may be x or residual."""
+    what = "jenga_rms_norm"
+    x_type, y_type = _type(x, what), _type(y, what)
+    shape, dtype = x.shape, x.dtype
+    x_row, x_head = _heads(x, what)
+    rows, cols = shape[0], shape[-1]
+    add_row = add_head = sum_row = sum_head = y_row = y_head = 0
+    if residual is not None:
+        add_row, add_head = _heads(residual, what, shape, dtype)
+    if total is not None:
+        sum_row, sum_head = _heads(total, what, shape, dtype)
+    if y_type == JENGA_E4M3:
+        padded = padded_columns(cols)
+        if len(shape) != 2 or y_scale is None:
+            _refuse(what, "results in 8 and 4 bits are of [rows, cols], with scales")
+        if y.dtype is _DTYPE["u8"]:
+            y_type = JENGA_E2M1
+            _whole(y, what, (rows, padded // 2), "u8")
+            _whole(y_scale, what, (rows, padded // 32), "u8")
+        else:
+            _whole(y, what, (rows, padded), "e4m3")
+            _whole(y_scale, what, (rows, scale_columns(cols)), "u8")
+    else:
+        y_row, y_head = _heads(y, what, shape, dtype)
+        if y_scale is not None:
+            _refuse(what, "scales of a result that has none")
+    param_type = x_type
+    if weight is not None:
+        param_type = _type(weight, what)
+        if weight.shape != shape[-1:] or weight.stride()[0] != 1 and cols != 1:
+            _refuse(what, "weight of shape %s" % (tuple(weight.shape),))
+    if rstd is not None:
+        _whole(rstd, what, shape[:-1], "f32")
+    stream = _on_device(what, (x, y, weight, residual, total, y_scale, rstd), stream)
+    if rows and (len(shape) == 2 or shape[1]):
+        cfg = _pack(what, _RMS, rows, x_row, x_head, add_row, add_head, sum_row, sum_head, y_row, y_head, shape[1] if len(shape) == 3 else 1,
+                    cols, x_type, y_type, param_type, eps, weight_offset, 0)
+        _check(_lib.jenga_rms_norm(cfg, x.data_ptr(), None if residual is None else residual.data_ptr(),
+                                   None if weight is None else weight.data_ptr(), None if total is None else total.data_ptr(), y.data_ptr(),
+                                   None if y_scale is None else y_scale.data_ptr(), None if rstd is None else rstd.data_ptr(), stream), what)
+
+
+def jenga_rms_norm_grad_workspace(rows, cols):
+    """Bytes of the workspace of jenga_rms_norm_grad; rows: with their heads."""
+    bytes_ = ctypes.c_uint64()
+    cfg = _pack("jenga_rms_norm_grad_workspace", _RMS, rows, cols, cols, 0, 0, 0, 0, cols, cols, 1, cols, JENGA_F32, JENGA_F32, JENGA_F32,
+                0.0, 0.0, 0)
+    _check(_lib.jenga_rms_norm_grad_workspace(cfg, ctypes.byref(bytes_)), "jenga_rms_norm_grad_workspace")
+    return bytes_.value
+
+
+def jenga_rms_norm_grad(total, dy, dx, weight, rstd, dtotal=None, dweight=None, workspace=None, weight_offset=0.0, stream=None):
+    """Gradients of total (what was normed; the same for x and residual) and of weight, float32 [cols], from dy, jenga_rms_norm's rstd and
+    dtotal, the gradient that total has from elsewhere.  dx may be dtotal."""
+    what = "jenga_rms_norm_grad"
+    kind, shape, dtype = _type(total, what), total.shape, total.dtype
+    x_row, x_head = _heads(total, what)
+    y_row, y_head = _heads(dy, what, shape, dtype)
+    sum_row, sum_head = _heads(dx, what, shape, dtype)
+    rows, cols = shape[0], shape[-1]
+    add_row = add_head = 0
+    if dtotal is not None:
+        add_row, add_head = _heads(dtotal, what, shape, dtype)
+    param_type = kind
+    if weight is not None:
+        param_type = _type(weight, what)
+        if weight.shape != shape[-1:] or weight.stride()[0] != 1 and cols != 1:
+            _refuse(what, "weight of shape %s" % (tuple(weight.shape),))
+    if rstd is None:
+        _refuse(what, "rstd of the forward pass is wanted")
+    _whole(rstd, what, shape[:-1], "f32")
+    if dweight is not None:
+        _whole(dweight, what, shape[-1:], "f32")
+    stream = _on_device(what, (total, dy, dx, weight, rstd, dtotal, dweight, workspace), stream)
+    if rows and (len(shape) == 2 or shape[1]):
+        cfg = _pack(what, _RMS, rows, x_row, x_head, add_row, add_head, sum_row, sum_head, y_row, y_head, shape[1] if len(shape) == 3 else 1,
+                    cols, kind, kind, param_type, 0.0, weight_offset, 0)
+        _check(_lib.jenga_rms_norm_grad(cfg, total.data_ptr(), dy.data_ptr(), _ptr(weight), rstd.data_ptr(), _ptr(dtotal), dx.data_ptr(),
+                                        _ptr(dweight), _ptr(workspace),
+                                        0 if workspace is None else workspace.numel() * workspace.element_size(), stream), what)
+
+
+def jenga_dense_attn_workspace(q_rows, kv_rows, sequences, heads, kv_heads, head_dim):
+    """Bytes of the workspace of jenga_dense_attn for these numbers of rows, keys and sequences in all."""
+    bytes_ = ctypes.c_uint64()
+    cfg = _pack("jenga_dense_attn_workspace", _DENSE, q_rows, kv_rows, 0, 0, 0, 0, 0, 0, 0, 0, sequences, heads, kv_heads, head_dim,
+                JENGA_BF16, 0, 1.0, 0)
+    _check(_lib.jenga_dense_attn_workspace(cfg, ctypes.byref(bytes_)), "jenga_dense_attn_workspace")
+    return bytes_.value
+
+
+def jenga_dense_attn(q, k, v, out, q_start, kv_start, kv_len=None, causal=False, scale=None, workspace=None, stream=None):
+    """q, out [rows, heads, head_dim], k, v [keys, kv_heads, head_dim] (bf16 or fp16, any strides but the last); q_start, kv_start int32
+    [sequences + 1], kv_len int32 [sequences], on the device: rows and keys of each sequence.  out may be q.  scale: 1 / sqrt(head_dim)."""
+    what = "jenga_dense_attn"
+    kind, shape, keys, dtype = _type(q, what), q.shape, k.shape, q.dtype
+    if len(shape) != 3 or len(keys) != 3 or keys[2] != shape[2] or not shape[2]:
+        _refuse(what, "shapes %s, %s" % (tuple(shape), tuple(keys)))
+    q_row, q_head = _heads(q, what)
+    out_row, out_head = _heads(out, what, shape, dtype)
+    k_row, k_head = _heads(k, what, keys, dtype)
+    v_row, v_head = _heads(v, what, keys, dtype)
+    sequences = q_start.numel() - 1
+    if sequences < 0:
+        _refuse(what, "no starts")
+    _whole(q_start, what, (sequences + 1,), "i32")
+    _whole(kv_start, what, (sequences + 1,), "i32")
+    if kv_len is not None:
+        _whole(kv_len, what, (sequences,), "i32")
+    if workspace is None:
+        _refuse(what, "a workspace is wanted")
+    stream = _on_device(what, (q, k, v, out, q_start, kv_start, kv_len, workspace), stream)
+    if shape[0] and shape[1]:
+        cfg = _pack(what, _DENSE, shape[0], keys[0], q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head, sequences, shape[1],
+                    keys[1], shape[2], kind, JENGA_DENSE_CAUSAL if causal else 0, shape[2] ** -0.5 if scale is None else scale, 0)
+        # without keys there is nothing to read, but the call wants addresses
+        here = q.data_ptr()
+        _check(_lib.jenga_dense_attn(cfg, here, k.data_ptr() or here, v.data_ptr() or here, q_start.data_ptr(), kv_start.data_ptr(),
+                                     None if kv_len is None else kv_len.data_ptr(), out.data_ptr(), workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), stream), what)
 
 
 def make_rotary(T, H, W, head_dim, dims, theta=10000.0, origin=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0), flags=0):

@@ -1,0 +1,797 @@
+// Softmax attention of packed sequences to all of their keys, causal or not, with heads that share keys.
+//
+//   o_i = sum over j of p_ij v_j / sum over j of p_ij,   p_ij = 2^(c q_i k_j - m_i),   c = scale log2(e)
+//
+// The rows of a sequence and of the heads that share keys are packed: row n is token n / group, head n % group.  A tile of packed rows walks
+// its keys once; the reference m_i of a row moves only when the sum of a step leaves its range (see SUM_MAX), and cancels.  The transposed
+// products S^T = K Q^T and O^T = V^T P^T keep a row in one lane of every accumulator, and the accumulators of S^T are the operand of
+// the second product as they are.
+//
+// Three launches: the list of work from the lengths, which are on the device; the tiles, of which long ones are cut along their keys where
+// there are few; and, if some may be, the joining of their parts in the order of the keys.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "jenga_device.h"
+#include "jenga_internal.h"
+#include "jenga_tiles.h"
+
+namespace {
+
+using namespace jenga;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+struct DenseArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t* out;
+  const int32_t *q_start, *kv_start, *kv_len;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+  int32_t q_rows, kv_rows, sequences, kv_heads, group;
+  uint32_t by_group, group_shift;
+  int32_t causal;
+  float scale_log2e;
+  int32_t tile, keys, max_tiles, workgroups, may_split;   // keys: of a step
+  int32_t *counts, *bins;   // items and merges; tiles of the sequences in front of each
+  DenseItem* items;
+  DenseMerge* merges;
+  float *stat, *part;       // [slot][kv_heads][tile][2]: reference, sum; [slot][kv_heads][tile][D]
+};
+
+// ---- the two types
+
+template <typename T>
+struct Type;
+template <>
+struct Type<__bf16> {
+  typedef bf16x8 eight;
+  static constexpr float SUM_MAX = 1073741824.0f;   // 2^30
+  static constexpr uint32_t EXPONENT = 0x7F807F80u;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const f32x2 v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+  }
+  static __device__ __forceinline__ f32x16 mul32(const eight& a, const eight& b, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+#endif
+    return c;
+  }
+  static __device__ __forceinline__ f32x4 mul16(const eight& a, const eight& b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+#endif
+    return c;
+  }
+};
+template <>
+struct Type<_Float16> {
+  typedef f16x8 eight;
+  static constexpr float SUM_MAX = 32768.0f;   // below the largest fp16
+  static constexpr uint32_t EXPONENT = 0x7C007C00u;
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const f32x2 v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+  }
+  static __device__ __forceinline__ f32x16 mul32(const eight& a, const eight& b, f32x16 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+#endif
+    return c;
+  }
+  static __device__ __forceinline__ f32x4 mul16(const eight& a, const eight& b, f32x4 c) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+#endif
+    return c;
+  }
+};
+
+// Whether one of the 16-bit values is an infinity or a NaN: a halfword whose exponent bits are all set.
+template <typename T>
+__device__ __forceinline__ bool not_finite(uint32_t w) {
+  const uint32_t v = (w & Type<T>::EXPONENT) ^ Type<T>::EXPONENT;
+  return ((v - 0x00010001u) & ~v & 0x80008000u) != 0;
+}
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Four rows x 16 channels of 16 bits, a row by four lanes of 8 bytes, to the 16 lanes of a group: lane i gets channel i, row 0 first.
+__device__ __forceinline__ u32x2 columns(uint32_t lds) {
+  u32x2 r = {};
+#if defined(__HIP_DEVICE_COMPILE__)
+  r = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)lds));
+#endif
+  return r;
+}
+__device__ __forceinline__ u32x4 piece16(uint32_t lds) {
+  return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)lds;
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+__device__ __forceinline__ uint32_t token_of(const DenseArgs& a, uint32_t row) {   // row / group, exact below 2^31
+  return a.group == 1 ? row : (__umulhi(row, a.by_group) + row) >> a.group_shift;
+}
+
+// ---- the list of work
+
+struct Lengths {
+  int q0, nq, kv0, nk;
+};
+__device__ __forceinline__ Lengths lengths_of(const DenseArgs& a, int s) {
+  Lengths n;
+  n.q0 = min(max(a.q_start[s], 0), a.q_rows);
+  n.nq = max(min(max(a.q_start[s + 1], 0), a.q_rows) - n.q0, 0);
+  n.kv0 = min(max(a.kv_start[s], 0), a.kv_rows);
+  n.nk = a.kv_len ? min(max(a.kv_len[s], 0), a.kv_rows - n.kv0) : max(min(max(a.kv_start[s + 1], 0), a.kv_rows) - n.kv0, 0);
+  return n;
+}
+__device__ __forceinline__ int keys_of_tile(const DenseArgs& a, const Lengths& n, int row0) {
+  if (!a.causal) return n.nk;
+  const int last = min((int)token_of(a, (uint32_t)row0 + a.tile - 1), n.nq - 1);
+  return max(0, min(n.nk, (int)min((int64_t)last + 1 + n.nk - n.nq, (int64_t)n.nk)));
+}
+
+// Sum over the threads in front; *total: over all of them.
+__device__ __forceinline__ int64_t scan(int64_t v, int64_t* room, int64_t* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t s = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t x = __shfl_up(s, o);
+    if (lane >= o) s += x;
+  }
+  __syncthreads();   // the room is free
+  if (lane == 63) room[wave] = s;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) before += room[w];
+    all += room[w];
+  }
+  *total = all;
+  return before + s - v;
+}
+// The last of n ascending numbers that is not above x; the first one is not.
+__device__ __forceinline__ int last_below(const int32_t* p, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (p[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(1024) void dense_plan_kernel(DenseArgs a) {
+  constexpr int IN_LDS = 4096;
+  __shared__ int64_t room[16];
+  __shared__ int32_t bins_here[IN_LDS];
+  __shared__ int32_t of_tile[1024][3];   // steps, first item, first slot
+  __shared__ int32_t first_item[1025];
+  const int tid = threadIdx.x;
+  int32_t* bins = a.sequences <= IN_LDS ? bins_here : a.bins;
+  int64_t tiles = 0, total;
+  for (int s0 = 0; s0 < a.sequences; s0 += 1024) {
+    const int s = s0 + tid;
+    int64_t n = 0;
+    if (s < a.sequences) n = ((int64_t)lengths_of(a, s).nq * a.group + a.tile - 1) / a.tile;
+    const int64_t before = tiles + scan(n, room, &total);
+    if (s < a.sequences) bins[s] = (int32_t)min(before, (int64_t)a.max_tiles);
+    tiles += total;
+  }
+  __syncthreads();
+  auto tile_at_index = [&](int j, DenseItem* item) {
+    const int s = last_below(bins, a.sequences, j);
+    const Lengths n = lengths_of(a, s);
+    item->q0 = n.q0;
+    item->nq = n.nq;
+    item->kv0 = n.kv0;
+    item->nk = n.nk;
+    item->row0 = (j - bins[s]) * a.tile;
+    item->begin = 0;
+    item->end = keys_of_tile(a, n, item->row0);
+    item->slot = -1;
+  };
+  const int n_tiles = (int)min(tiles, (int64_t)a.max_tiles);   // more only where starts do not ascend
+  if (!a.may_split || tiles * a.kv_heads >= a.workgroups) {
+    for (int j = tid; j < n_tiles; j += 1024) {
+      DenseItem item;
+      tile_at_index(j, &item);
+      a.items[j] = item;
+    }
+    if (tid == 0) a.counts[0] = n_tiles, a.counts[1] = 0;
+    return;
+  }
+  // fewer tiles than workgroups wanted (1024 at most): cut into parts of equal length
+  DenseItem mine = {};
+  int steps = 0;
+  if (tid < n_tiles) {
+    tile_at_index(tid, &mine);
+    steps = (mine.end + a.keys - 1) / a.keys;
+  }
+  int64_t all;
+  scan(steps, room, &all);
+  const int chunk = (int)max((all * a.kv_heads + a.workgroups - 1) / a.workgroups, (int64_t)1);
+  const int parts = tid < n_tiles ? max((steps + chunk - 1) / chunk, 1) : 0;
+  int64_t n_items, n_slots, n_merges;
+  const int item0 = (int)scan(parts, room, &n_items);
+  const int slot0 = (int)scan(parts > 1 ? parts : 0, room, &n_slots);
+  const int merge0 = (int)scan(parts > 1 ? 1 : 0, room, &n_merges);
+  if (tid < n_tiles) {
+    of_tile[tid][0] = steps;
+    of_tile[tid][1] = parts;
+    of_tile[tid][2] = parts > 1 ? slot0 : -1;
+    first_item[tid] = item0;
+    if (parts > 1) a.merges[merge0] = {mine.q0, mine.nq, mine.row0, slot0, parts, 0};
+  }
+  __syncthreads();
+  for (int i = tid; i < n_items; i += 1024) {
+    const int j = last_below(first_item, n_tiles, i);
+    DenseItem item;
+    tile_at_index(j, &item);
+    const int part = i - first_item[j], n = of_tile[j][1], st = of_tile[j][0];
+    item.begin = (int)((int64_t)st * part / n) * a.keys;
+    item.end = min(item.end, (int)((int64_t)st * (part + 1) / n) * a.keys);
+    item.slot = of_tile[j][2] < 0 ? -1 : of_tile[j][2] + part;
+    a.items[i] = item;
+  }
+  if (tid == 0) a.counts[0] = (int)n_items, a.counts[1] = (int)n_merges;
+}
+
+// ---- tiles of 128 rows
+
+// What a lane's row is: its token's place in q and out, how many keys it sees.
+struct Row {
+  int64_t token;   // of all
+  int head, limit;
+  bool there;
+};
+__device__ __forceinline__ Row row_at(const DenseArgs& a, const DenseItem& it, int kv_head, int row) {
+  const uint32_t t = token_of(a, (uint32_t)row);
+  Row r;
+  r.there = (int)t < it.nq;
+  const int token = min((int)t, it.nq - 1);
+  r.head = kv_head * a.group + (row - (int)t * a.group);
+  r.token = (int64_t)it.q0 + token;
+  r.limit = a.causal ? (int)min((int64_t)token + 1 + it.nk - it.nq, (int64_t)it.end) : it.end;
+  return r;
+}
+
+// The keys of a step as a buffer: what lies behind them reads as 0.
+__device__ __forceinline__ u32x4 keys_of_step(const uint16_t* base, int64_t row_stride, int64_t first, int count, int D) {
+  return buffer_of((const uint8_t*)(base + first * row_stride), (uint32_t)(((count - 1) * row_stride + D) * 2));
+}
+
+// ALIGNED: rows of k and v on the 16-byte grid, which the copies into LDS want.
+//
+// SUM_MAX: a step forms its probabilities against the reference as it stands and only looks at their sum.  While a lane's 32 add up to at
+// most SUM_MAX, they, their float32 sums and the float32 products made of them can all be represented.  A sum above it, infinite or
+// undefined sends the step down the exact path: logits again, the row's maximum, what has been added up rescaled, probabilities <= 1.  The first
+// step of a row starts there, so the reference never exceeds the largest logit seen and the largest term is never lost to underflow.
+template <typename T, int D, bool ALIGNED>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dense_tiles_kernel(DenseArgs a) {
+  typedef typename Type<T>::eight eight;
+  constexpr int KEYS = 64, KS = D / 16, DT = D / 32, MH = KEYS / 32, PH = KEYS / 16, CH = D / 8;
+  constexpr int CHUNKS = KEYS * CH, COPIES = CHUNKS / 256, ROWS_PER_COPY = 256 / CH;
+  __shared__ __attribute__((aligned(256))) u32x4 Ks[CHUNKS];
+  __shared__ __attribute__((aligned(256))) u32x4 Vs[CHUNKS];
+  const int index = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - index * a.kv_heads;
+  if (index >= a.counts[0]) return;
+  const DenseItem it = a.items[index];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hl = lane >> 5, ql = lane & 31;
+  int row = it.row0 + 32 * wave + ql;
+  Row r = row_at(a, it, kv_head, row);
+  // keys that all rows of the tile see
+  const int first_token = (int)token_of(a, (uint32_t)it.row0);
+  const int all_see = a.causal ? (int)min((int64_t)first_token + 1 + it.nk - it.nq, (int64_t)it.end) : it.end;
+
+  eight qf[KS];
+  {
+    const uint16_t* qp = a.q + r.token * a.q_row + (int64_t)r.head * a.q_head + 8 * hl;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const Piece16 p = *(const Piece16*)(qp + 16 * ks);
+      __builtin_memcpy(&qf[ks], &p, 16);
+    }
+  }
+
+  // The 16-byte pieces of a row are rotated by an exclusive or on the way.  K: so that the 16 rows that are read at a time fall on different
+  // banks.  V is read by columns, which hands a lane four keys of its channel: two of them are a fragment, in the key order of the accumulators.
+  auto k_swizzle = [](int n) { return D == 128 ? n & 15 : (n >> 1) & 7; };
+  auto v_swizzle = [](int n) { return D == 128 ? (n & 3) * 4 : (n & 2) * 2; };
+  const int copy_row = tid / CH, copy_piece = tid % CH;
+  const uint32_t k_from = (uint32_t)copy_row * (uint32_t)a.k_row * 2 + (copy_piece ^ k_swizzle(copy_row)) * 16;
+  const uint32_t v_from = (uint32_t)copy_row * (uint32_t)a.v_row * 2 + (copy_piece ^ v_swizzle(copy_row)) * 16;
+  const uint16_t *k0 = a.k + (int64_t)it.kv0 * a.k_row + kv_head * a.k_head, *v0 = a.v + (int64_t)it.kv0 * a.v_row + kv_head * a.v_head;
+  const uint32_t ks_wave = lds_address(Ks) + wave * 1024, vs_wave = lds_address(Vs) + wave * 1024;
+  auto copy = [&](const uint16_t* base, int64_t stride, uint32_t from, u32x4* to, uint32_t lds, int key) {
+    const u32x4 rows = keys_of_step(base, stride, key, min(KEYS, it.end - key), D);
+    if constexpr (ALIGNED) {
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c) copy_1kb(rows, from, (uint32_t)(c * ROWS_PER_COPY) * (uint32_t)stride * 2, lds + c * 4096);
+    } else {
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c) {
+        const int n = copy_row + c * ROWS_PER_COPY;
+        Piece16 p = {};
+        if (key + n < it.end) p = *(const Piece16*)((const uint8_t*)(base + (int64_t)key * stride) + from + (int64_t)c * ROWS_PER_COPY * stride * 2);
+        to[tid + c * 256] = (u32x4){p.w[0], p.w[1], p.w[2], p.w[3]};
+      }
+    }
+  };
+  auto landed = []() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); };
+
+  float m_run = r.limit > it.begin ? -__builtin_inff() : 0.f, l_run = 0.f;   // 0: a row that sees none of these keys
+  bool unset = true;
+  f32x16 O[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) O[dt] = 0.f;
+
+  const uint32_t ks_lane = lds_address(Ks) + ql * (2 * D) + (hl ^ k_swizzle(ql)) * 16;
+  const int v_row = 4 * hl + ((lane >> 2) & 3);
+  const uint32_t vs_lane = lds_address(Vs) + v_row * (2 * D) + v_swizzle(v_row) * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+
+  if (it.begin < it.end) copy(k0, a.k_row, k_from, Ks, ks_wave, it.begin);
+  for (int key = it.begin; key < it.end; key += KEYS) {
+    landed();
+    __syncthreads();   // K of this step is in LDS; every wavefront is past the products of the step before
+    copy(v0, a.v_row, v_from, Vs, vs_wave, key);
+    const bool masked = key + KEYS > all_see;
+    f32x16 S[MH];
+    auto logits = [&]() {
+#pragma unroll
+      for (int m = 0; m < MH; ++m) S[m] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int m = 0; m < MH; ++m)
+          S[m] = Type<T>::mul32(__builtin_bit_cast(eight, piece16((ks_lane ^ (ks * 32)) + m * 64 * D)), qf[ks], S[m]);
+      if (masked) {
+        const int left = r.limit - key - 4 * hl;
+#pragma unroll
+        for (int m = 0; m < MH; ++m)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (32 * m + 8 * (e / 4) + e % 4 >= left) S[m][e] = -__builtin_inff();
+      }
+    };
+    eight pb[PH];
+    auto probabilities = [&](float off) {
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int p = 0; p < PH; ++p) {
+        u32x4 w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p0 = exp2_of(fmaf(S[p >> 1][8 * (p & 1) + 2 * e], a.scale_log2e, off));
+          const float p1 = exp2_of(fmaf(S[p >> 1][8 * (p & 1) + 2 * e + 1], a.scale_log2e, off));
+          w[e] = Type<T>::pack(p0, p1);
+          s0 += p0;
+          s1 += p1;
+        }
+        pb[p] = __builtin_bit_cast(eight, w);
+      }
+      return s0 + s1;
+    };
+    float sum = 0.f;
+    bool in_range = false;
+    if (!unset) {
+      logits();
+      sum = probabilities(-m_run);
+      in_range = __ballot(!(sum <= Type<T>::SUM_MAX)) == 0;
+    }
+    if (!in_range) {
+      logits();
+      float top = -__builtin_inff();
+#pragma unroll
+      for (int m = 0; m < MH; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, S[m][e]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m_new = fmaxf(m_run, top * a.scale_log2e);
+      const float alpha = m_new == m_run ? 1.0f : exp2_of(m_run - m_new);
+      l_run *= alpha;
+      m_run = m_new;
+      unset = __ballot(m_run == -__builtin_inff()) != 0;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) O[dt] *= alpha;
+      sum = probabilities(m_run == -__builtin_inff() ? 0.f : -m_run);
+    }
+    l_run += sum;
+    landed();
+    __syncthreads();   // V is in LDS; every wavefront has read K
+    if (key + KEYS < it.end) copy(k0, a.k_row, k_from, Ks, ks_wave, key + KEYS);
+    auto v_fragment = [&](int dt, int p) {
+      const uint32_t at = (vs_lane ^ (dt * 64)) + p * 32 * D;
+      const u32x2 lo = columns(at), hi = columns(at + 16 * D);
+      return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+    };
+    // Keys that some rows do not see have probability 0 there, which is not enough where their values are not finite.
+    bool careful = false;
+    if (masked && a.causal) {
+      uint32_t found = 0;
+#pragma unroll 4
+      for (int i = lane; i < CHUNKS; i += 64) {
+        const u32x4 w = piece16(lds_address(Vs) + i * 16);
+        found |= not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
+      }
+      careful = __ballot(found != 0) != 0;
+    }
+    if (!careful) {
+#pragma unroll
+      for (int p = 0; p < PH; ++p)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul32(__builtin_bit_cast(eight, v_fragment(dt, p)), pb[p], O[dt]);
+    } else {   // a key at a time, and only for the rows that see it
+#pragma unroll
+      for (int p = 0; p < PH; ++p)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const u32x4 v = v_fragment(dt, p);
+#pragma unroll 1
+          for (int e = 0; e < 16; ++e) {
+            const int i = e & 7, half = e >> 3;
+            u32x4 one = 0u;
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              if (w == i >> 1 && half == hl) one[w] = v[w] & (i & 1 ? 0xFFFF0000u : 0xFFFFu);
+            const f32x16 with = Type<T>::mul32(__builtin_bit_cast(eight, one), pb[p], O[dt]);
+            if (key + 16 * p + 8 * (i >> 2) + 4 * half + (i & 3) < r.limit) O[dt] = with;
+          }
+        }
+    }
+  }
+
+  // lane holds channels 32 dt + 8 g + 4 hl + 0..3 of its row
+  const float l_all = l_run + __shfl_xor(l_run, 32);
+  if (it.slot >= 0) {
+    if (!r.there) return;
+    const int64_t at = ((int64_t)it.slot * a.kv_heads + kv_head) * 128 + 32 * wave + ql;
+    float* o = a.part + at * D + 4 * hl;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) *(float4*)(o + 32 * dt + 8 * g) = make_float4(O[dt][4 * g], O[dt][4 * g + 1], O[dt][4 * g + 2], O[dt][4 * g + 3]);
+    if (hl == 0) a.stat[2 * at] = m_run, a.stat[2 * at + 1] = l_all;
+    return;
+  }
+  if (!r.there) return;
+  const float inv = l_all > 0.f ? 1.0f / l_all : l_all == 0.f ? 0.f : l_all;   // NaN stays
+  uint16_t* out = a.out + r.token * a.out_row + (int64_t)r.head * a.out_head + 4 * hl;
+  struct __attribute__((packed, aligned(2))) Piece8 {
+    uint32_t w[2];
+  };
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      Piece8 w = {{Type<T>::pack(O[dt][4 * g] * inv, O[dt][4 * g + 1] * inv), Type<T>::pack(O[dt][4 * g + 2] * inv, O[dt][4 * g + 3] * inv)}};
+      *(Piece8*)(out + 32 * dt + 8 * g) = w;
+    }
+}
+
+// ---- tiles of 16 rows
+
+// Few rows: the keys are read once and are what takes the time.  Each of the four wavefronts takes 32 keys of every 128 with LDS of its own,
+// two steps deep, so that nothing but its own copies makes it wait; the four join at the end.
+template <typename T, int D, bool ALIGNED>
+__global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
+  typedef typename Type<T>::eight eight;
+  constexpr int KEYS = 32, KS = D / 32, DT = D / 16, CH = D / 8, BYTES = KEYS * D * 2, STAGES = 2;
+  constexpr int COPIES = BYTES / 1024, ROWS_PER_COPY = 64 / CH;   // of a wavefront, for K
+  constexpr int ROOM = STAGES * 2 * BYTES;                        // of a wavefront
+  __shared__ __attribute__((aligned(256))) uint8_t tiles[4 * ROOM];
+  __shared__ float stats[4][16][2];
+  static_assert(ROOM >= 16 * D * 4, "");
+  const int index = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - index * a.kv_heads;
+  if (index >= a.counts[0]) return;
+  const DenseItem it = a.items[index];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, i16 = lane & 15;
+  const Row r = row_at(a, it, kv_head, it.row0 + i16);
+  const int first_token = (int)token_of(a, (uint32_t)it.row0);
+  const int all_see = a.causal ? (int)min((int64_t)first_token + 1 + it.nk - it.nq, (int64_t)it.end) : it.end;
+  eight qf[KS];
+  {
+    const uint16_t* qp = a.q + r.token * a.q_row + (int64_t)r.head * a.q_head + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const Piece16 p = *(const Piece16*)(qp + 32 * ks);
+      __builtin_memcpy(&qf[ks], &p, 16);
+    }
+  }
+  auto k_swizzle = [](int n) { return D == 128 ? n & 15 : (n >> 1) & 7; };
+  auto v_swizzle = [](int n) { return D == 128 ? (n & 3) * 4 : (n & 2) * 2; };
+  const int copy_row = lane / CH, copy_piece = lane % CH;
+  const uint16_t *k0 = a.k + (int64_t)it.kv0 * a.k_row + kv_head * a.k_head, *v0 = a.v + (int64_t)it.kv0 * a.v_row + kv_head * a.v_head;
+  const uint32_t lds = lds_address(tiles) + wave * ROOM;
+  auto copy = [&](const uint16_t* base, int64_t stride, auto swizzle, int key, uint32_t to) {
+    const int left = it.end - key;
+    const u32x4 rows = keys_of_step(base, stride, left > 0 ? key : it.begin, max(min(KEYS, left), 1), D);
+#pragma unroll
+    for (int c = 0; c < COPIES; ++c) {
+      const int n = c * ROWS_PER_COPY;
+      const uint32_t from = (uint32_t)copy_row * (uint32_t)stride * 2 + (copy_piece ^ swizzle(copy_row) ^ swizzle(n)) * 16;
+      if constexpr (ALIGNED) {
+        copy_1kb(rows, from, left > 0 ? (uint32_t)n * (uint32_t)stride * 2 : 0x80000000u, to + c * 1024);   // past the end: outside
+      } else {
+        Piece16 p = {};
+        if (n + copy_row < left) p = *(const Piece16*)((const uint8_t*)(base + (int64_t)(key + n) * stride) + from);
+        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + c * 1024 + lane * 16) = (u32x4){p.w[0], p.w[1], p.w[2], p.w[3]};
+      }
+    }
+  };
+  auto copy_step = [&](int key, int stage) {
+    copy(k0, a.k_row, k_swizzle, key, lds + stage * 2 * BYTES);
+    copy(v0, a.v_row, v_swizzle, key, lds + stage * 2 * BYTES + BYTES);
+  };
+  float m_run = r.limit > it.begin ? -__builtin_inff() : 0.f, l_run = 0.f;
+  bool unset = true;
+  f32x4 O[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) O[dt] = 0.f;
+  const uint32_t k_lane = i16 * (2 * D) + (g ^ k_swizzle(i16)) * 16;
+  const int v_row = 4 * g + ((lane >> 2) & 3);
+  const uint32_t v_lane = BYTES + v_row * (2 * D) + (((lane >> 1) & 1) ^ v_swizzle(v_row)) * 16 + (lane & 1) * 8;
+
+  int key = it.begin + KEYS * wave, stage = 0;
+  if (key < it.end) {
+    copy_step(key, 0);
+    copy_step(key + 4 * KEYS, 1);
+  }
+  for (; key < it.end; key += 4 * KEYS, stage ^= 1) {
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(ALIGNED ? 2 * COPIES : 0) : "memory");
+    const uint32_t at = lds + stage * 2 * BYTES;
+    const bool masked = key + KEYS > all_see;
+    f32x4 S[2] = {};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+        S[m] = Type<T>::mul16(__builtin_bit_cast(eight, piece16(at + (k_lane ^ (ks * 64)) + m * 32 * D)), qf[ks], S[m]);
+    if (masked) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (key + 16 * m + 4 * g + e >= r.limit) S[m][e] = -__builtin_inff();
+    }
+    eight pb;
+    auto probabilities = [&](float off) {
+      float s = 0.f;
+      u32x4 w;
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = exp2_of(fmaf(S[m][e], a.scale_log2e, off));
+          s += p[e];
+        }
+        w[2 * m] = Type<T>::pack(p[0], p[1]);
+        w[2 * m + 1] = Type<T>::pack(p[2], p[3]);
+      }
+      pb = __builtin_bit_cast(eight, w);
+      return s;
+    };
+    float sum = 0.f;
+    bool in_range = false;
+    if (!unset) {
+      sum = probabilities(-m_run);
+      in_range = __ballot(!(sum <= Type<T>::SUM_MAX)) == 0;
+    }
+    if (!in_range) {
+      float top = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m_new = fmaxf(m_run, top * a.scale_log2e);
+      const float alpha = m_new == m_run ? 1.0f : exp2_of(m_run - m_new);
+      l_run *= alpha;
+      m_run = m_new;
+      unset = __ballot(m_run == -__builtin_inff()) != 0;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) O[dt] *= alpha;
+      sum = probabilities(m_run == -__builtin_inff() ? 0.f : -m_run);
+    }
+    l_run += sum;
+    // channels 16 dt to + 15: pieces 2 dt and 2 dt + 1 of the row, before their rotation
+    auto v_fragment = [&](int dt) {
+      const uint32_t from = at + (v_lane ^ (dt * 32));
+      const u32x2 lo = columns(from), hi = columns(from + 32 * D);
+      return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+    };
+    bool careful = false;
+    if (masked && a.causal) {
+      uint32_t found = 0;
+#pragma unroll
+      for (int i = 0; i < COPIES; ++i) {
+        const u32x4 w = piece16(at + BYTES + i * 1024 + lane * 16);
+        found |= not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
+      }
+      careful = __ballot(found != 0) != 0;
+    }
+    if (!careful) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul16(__builtin_bit_cast(eight, v_fragment(dt)), pb, O[dt]);
+    } else {   // a key at a time, and only for the rows that see it
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const u32x4 v = v_fragment(dt);
+#pragma unroll 1
+        for (int e = 0; e < 32; ++e) {
+          const int i = e & 7, of = e >> 3;
+          u32x4 one = 0u;
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            if (w == i >> 1 && of == g) one[w] = v[w] & (i & 1 ? 0xFFFF0000u : 0xFFFFu);
+          const f32x4 with = Type<T>::mul16(__builtin_bit_cast(eight, one), pb, O[dt]);
+          if (key + 16 * (i >> 2) + 4 * of + (i & 3) < r.limit) O[dt] = with;
+        }
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // this stage has been read
+    copy_step(key + 8 * KEYS, stage);
+  }
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");   // nothing is on its way into LDS
+
+  // the four wavefronts' results
+  l_run += __shfl_xor(l_run, 16);
+  l_run += __shfl_xor(l_run, 32);
+  if (lane < 16) stats[wave][i16][0] = m_run, stats[wave][i16][1] = l_run;
+  float* mine = (float*)(tiles + wave * ROOM) + i16 * D + 4 * g;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) *(f32x4*)(mine + 16 * dt) = O[dt];
+  __syncthreads();
+  const int row = tid >> 4, c0 = (tid & 15) * (D / 16);   // a thread: D / 16 channels of a row
+  const Row to = row_at(a, it, kv_head, it.row0 + row);
+  if (!to.there) return;
+  float m_all = -__builtin_inff(), l_all = 0.f, o[D / 16] = {};
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+    if (stats[w][row][1] != 0.f) m_all = fmaxf(m_all, stats[w][row][0]);   // NaN is not 0
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float l = stats[w][row][1];
+    if (l == 0.f) continue;
+    const float by = exp2_of(stats[w][row][0] - m_all);
+    l_all = fmaf(l, by, l_all);
+    const float* from = (const float*)(tiles + w * ROOM) + row * D + c0;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i] = fmaf(from[i], by, o[i]);
+  }
+  if (it.slot >= 0) {
+    const int64_t n = ((int64_t)it.slot * a.kv_heads + kv_head) * 16 + row;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) a.part[n * D + c0 + i] = o[i];
+    if ((tid & 15) == 0) a.stat[2 * n] = l_all == 0.f ? 0.f : m_all, a.stat[2 * n + 1] = l_all;
+    return;
+  }
+  const float inv = l_all > 0.f ? 1.0f / l_all : l_all == 0.f ? 0.f : l_all;
+  T* out = (T*)a.out + to.token * a.out_row + (int64_t)to.head * a.out_head + c0;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) out[i] = (T)(o[i] * inv);
+}
+
+// ---- joining
+
+// A workgroup a tile that was cut: the parts in their order, relative to the largest reference.
+template <typename T, int D, int TILE>
+__global__ __launch_bounds__(256) void dense_merge_kernel(DenseArgs a) {
+  __shared__ float tops[TILE], invs[TILE];
+  const int index = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - index * a.kv_heads;
+  if (index >= a.counts[1]) return;
+  const DenseMerge it = a.merges[index];
+  const int64_t first = ((int64_t)it.slot * a.kv_heads + kv_head) * TILE, step = (int64_t)a.kv_heads * TILE;
+  const int rows = min(TILE, it.nq * a.group - it.row0);
+  if ((int)threadIdx.x < rows) {
+    const float* s = a.stat + 2 * (first + threadIdx.x);
+    float top = -__builtin_inff(), l = 0.f;
+    for (int p = 0; p < it.parts; ++p)
+      if (s[2 * step * p + 1] != 0.f) top = fmaxf(top, s[2 * step * p]);
+    for (int p = 0; p < it.parts; ++p)
+      if (s[2 * step * p + 1] != 0.f) l = fmaf(s[2 * step * p + 1], exp2_of(s[2 * step * p] - top), l);
+    tops[threadIdx.x] = top;
+    invs[threadIdx.x] = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
+    const int row = i / (D / 4), c = i % (D / 4) * 4;
+    f32x4 o = 0.f;
+    for (int p = 0; p < it.parts; ++p) {
+      const int64_t n = first + step * p + row;
+      if (a.stat[2 * n + 1] != 0.f) o += *(const f32x4*)(a.part + n * D + c) * exp2_of(a.stat[2 * n] - tops[row]);
+    }
+    const uint32_t t = token_of(a, (uint32_t)(it.row0 + row));
+    const int head = kv_head * a.group + it.row0 + row - (int)t * a.group;
+    T* out = (T*)a.out + ((int64_t)it.q0 + t) * a.out_row + (int64_t)head * a.out_head + c;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (T)(o[e] * invs[row]);
+  }
+}
+
+int status() { return hipGetLastError() == hipSuccess ? JENGA_OK : JENGA_EHIP; }
+
+template <typename T, int D, bool ALIGNED>
+int run(const DenseArgs& a, const DenseShape& s, hipStream_t st) {
+  const unsigned grid = (unsigned)(s.items * a.kv_heads), merges = (unsigned)(s.split_tiles * a.kv_heads);
+  dense_plan_kernel<<<1, 1024, 0, st>>>(a);
+  if (s.rows == 16) {
+    dense_rows_kernel<T, D, ALIGNED><<<grid, 256, 0, st>>>(a);
+    if (s.may_split) dense_merge_kernel<T, D, 16><<<merges, 256, 0, st>>>(a);
+  } else {
+    dense_tiles_kernel<T, D, ALIGNED><<<grid, 256, 0, st>>>(a);
+    if (s.may_split) dense_merge_kernel<T, D, 128><<<merges, 256, 0, st>>>(a);
+  }
+  return status();
+}
+
+}  // namespace
+
+extern "C" {
+
+int jenga_dense_attn(const jenga_dense_config* cfg, const void* q, const void* k, const void* v, const int32_t* q_start,
+                     const int32_t* kv_start, const int32_t* kv_len_or_null, void* out, void* workspace, size_t workspace_bytes,
+                     void* stream) {
+  const int why = jenga::dense_args_ok(cfg, q, k, v, q_start, kv_start, kv_len_or_null, out, workspace, workspace_bytes);
+  if (why != JENGA_OK) return why;
+  if (cfg->q_rows == 0 || cfg->sequences == 0) return JENGA_OK;
+  const DenseShape s = jenga::dense_shape(*cfg);
+  const jenga_dense_config& c = *cfg;
+  DenseArgs a = {};
+  a.q = (const uint16_t*)q;
+  a.k = (const uint16_t*)k;
+  a.v = (const uint16_t*)v;
+  a.out = (uint16_t*)out;
+  a.q_start = q_start;
+  a.kv_start = kv_start;
+  a.kv_len = kv_len_or_null;
+  a.q_row = c.q_row;
+  a.q_head = c.q_head;
+  a.k_row = c.k_row;
+  a.k_head = c.k_head;
+  a.v_row = c.v_row;
+  a.v_head = c.v_head;
+  a.out_row = c.out_row;
+  a.out_head = c.out_head;
+  a.q_rows = (int32_t)c.q_rows;
+  a.kv_rows = (int32_t)c.kv_rows;
+  a.sequences = c.sequences;
+  a.kv_heads = c.kv_heads;
+  a.group = c.heads / c.kv_heads;
+  int l = 0;
+  while ((1ll << l) < a.group) ++l;
+  a.group_shift = (uint32_t)l;
+  a.by_group = (uint32_t)((((1ull << l) - (uint64_t)a.group) << 32) / (uint64_t)a.group + 1);
+  a.causal = (c.flags & JENGA_DENSE_CAUSAL) != 0;
+  a.scale_log2e = c.scale * 1.4426950408889634f;
+  a.tile = s.rows;
+  a.keys = s.rows == 16 ? 128 : 64;
+  a.max_tiles = (int32_t)s.tiles;
+  a.workgroups = (int32_t)s.workgroups;
+  a.may_split = s.may_split;
+  uint8_t* ws = (uint8_t*)workspace;
+  a.counts = (int32_t*)ws;
+  a.bins = (int32_t*)(ws + s.bins_at);
+  a.items = (DenseItem*)(ws + s.items_at);
+  a.merges = (DenseMerge*)(ws + s.merge_at);
+  a.stat = (float*)(ws + s.stat_at);
+  a.part = (float*)(ws + s.part_at);
+  hipStream_t st = (hipStream_t)stream;
+  const bool aligned = (((uintptr_t)k | (uintptr_t)v) & 15) == 0 && (c.k_row | c.k_head | c.v_row | c.v_head) % 8 == 0;
+#define JENGA_DENSE(T)                                                                                     \
+  return c.head_dim == 128 ? (aligned ? run<T, 128, true>(a, s, st) : run<T, 128, false>(a, s, st))  \
+                           : (aligned ? run<T, 64, true>(a, s, st) : run<T, 64, false>(a, s, st))
+  if (c.type == JENGA_BF16) JENGA_DENSE(__bf16);
+  JENGA_DENSE(_Float16);
+#undef JENGA_DENSE
+}
+
+}  // extern "C"

@@ -165,4 +165,43 @@ __device__ __forceinline__ float largest_of(const f32x8& v) {
   return m;
 }
 
+// e2m1 with a power-of-two scale: values v of a block of 32 are kept as e2m1(v 2^-e), e the least whole number with max |v| <= 6 2^e
+// (0 where they are all zero), at least -127; the scale byte is e + 127, and 255 where a value is not finite.  Multiplying by a
+// power of two is exact, so the only rounding is the one to e2m1 (nearest, ties to even, v_cvt_scalef32_pk_fp4_f32).
+__device__ __forceinline__ float magnitude_of(const f32x8& v) {   // NaN wins
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = v[i];   // a bit cast of an element in its place takes the first one (clang 22)
+    m = max(m, __builtin_bit_cast(uint32_t, x) & 0x7FFFFFFFu);
+  }
+  return __builtin_bit_cast(float, m);
+}
+__device__ __forceinline__ float quad_max(float v) {   // over four neighbouring lanes, of magnitudes; NaN wins
+  auto bits = [](float f) { return __builtin_bit_cast(uint32_t, f); };
+  uint32_t m = max(bits(v), bits(dpp_f32<0xB1, 0xF>(0.f, v)));
+  m = max(m, bits(dpp_f32<0x4E, 0xF>(0.f, __builtin_bit_cast(float, m))));
+  return __builtin_bit_cast(float, m);
+}
+__device__ __forceinline__ uint32_t mx_scale_byte(float largest) {
+  const uint32_t bits = __builtin_bit_cast(uint32_t, largest);
+  if (bits == 0) return 127;
+  if (bits >= 0x7F800000u) return 255;
+  const int e = (int)(bits >> 23) - 2 + ((bits & 0x7FFFFFu) > 0x400000u ? 1 : 0);   // 6 = 1.5 * 2^2
+  return e < 0 ? 0u : (uint32_t)e;
+}
+// Eight values, the first in the lowest four bits.
+__device__ __forceinline__ uint32_t to_e2m1(const f32x8& v, uint32_t byte) {
+  uint32_t r = 0;
+#if defined(__HIP_DEVICE_COMPILE__)
+  const float inverse = inverse_scale(min(byte, 254u));
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[0] * inverse, v[1] * inverse, 1.0f, 0);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[2] * inverse, v[3] * inverse, 1.0f, 1);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[4] * inverse, v[5] * inverse, 1.0f, 2);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, v[6] * inverse, v[7] * inverse, 1.0f, 3);
+  if (byte == 255u) r = 0;   // its scale says it all
+#endif
+  return r;
+}
+
 }  // namespace jenga

@@ -92,6 +92,8 @@ MatmulTiles matmul_tiles(int64_t m, int64_t n, bool float32) {
   return {0, 128, 128, 2, 2};
 }
 
+MatmulTiles matmul_mx_tiles(int64_t m, int64_t n) { return matmul_tiles(m, n, false); }
+
 // ---- arguments of the calls around the attention
 
 namespace {
@@ -385,9 +387,244 @@ int rotary_args_ok(const jenga_rotary_config* c, const jenga_plan* plan, const i
   return JENGA_OK;
 }
 
+// ---- the norm without a mean, 4-bit products, dense attention
+
+namespace {
+
+constexpr int RMS_PARTS = 1024;   // workgroups that leave sums of the weight's gradient, at most
+
+// Rows and heads of a tensor as one of the calls sees them; null where there is none.
+Layout4 rows_and_heads(const void* at, int64_t row, int64_t head, int64_t rows, int64_t heads, int64_t width, int64_t size) {
+  return {at, 0, row, head, {1, rows, heads}, width, size};
+}
+bool same_place(const Layout4& a, const Layout4& b) {
+  return a.at == b.at && (a.n[1] == 1 || a.token == b.token) && (a.n[2] == 1 || a.head == b.head);
+}
+bool touch(const Layout4& a, const Layout4& b) { return a.at && b.at && share(a, b); }
+bool touch(const Layout4& a, const Span& b) { return a.at && overlap(a.rows(), b); }
+
+int rms_strides_ok(int64_t row, int64_t head, const jenga_rms_config& c) {
+  if (row < 0 || head < 0) return JENGA_EINVAL;
+  if (row > MOST_STRIDE || head > MOST_STRIDE) return JENGA_EUNSUPPORTED;
+  const __int128 lim = (__int128)1 << 60;
+  return (__int128)c.rows * row + (__int128)c.heads * head > lim ? JENGA_EUNSUPPORTED : JENGA_OK;
+}
+
+int rms_config_ok(const jenga_rms_config& c) {
+  if (c.rows < 0 || c.heads < 1 || c.cols < 1 || c.reserved != 0) return JENGA_EINVAL;
+  if (!float_type(c.x_type) || !float_type(c.param_type)) return JENGA_EINVAL;
+  if (!float_type(c.y_type) && c.y_type != JENGA_E4M3 && c.y_type != JENGA_E2M1) return JENGA_EINVAL;
+  if (!std::isfinite(c.eps) || c.eps < 0.0f || !std::isfinite(c.weight_offset)) return JENGA_EINVAL;
+  if (c.cols > MOST_COLS || c.rows > MOST_ROWS || c.heads > 1 << 20) return JENGA_EUNSUPPORTED;
+  if (c.heads > 1 && c.rows * c.heads >= 1ll << 31) return JENGA_EUNSUPPORTED;
+  if (float_type(c.y_type) ? c.y_type != c.x_type : c.heads != 1) return JENGA_EUNSUPPORTED;
+  if (c.param_type != c.x_type && c.param_type != JENGA_F32) return JENGA_EUNSUPPORTED;
+  return JENGA_OK;
+}
+
+}  // namespace
+
+int rms_args_ok(const jenga_rms_config* c, const void* x, const void* residual, const void* weight, const void* total, const void* y,
+                const uint8_t* y_scale, const float* rstd) {
+  if (!c || !x || !y) return JENGA_EINVAL;
+  int why = rms_config_ok(*c);
+  if (why != JENGA_OK) return why;
+  const int64_t xs = type_size(c->x_type), ps = type_size(c->param_type), blocks = ((int64_t)c->cols + 127) / 128;
+  const bool packed = !float_type(c->y_type);
+  const int64_t y_bytes = c->y_type == JENGA_E4M3 ? blocks * 128 : blocks * 64;
+  const int64_t scales = c->y_type == JENGA_E4M3 ? (blocks + 3) / 4 * 4 : blocks * 4;
+  if (packed != (y_scale != nullptr) || (packed && (!aligned(y, 16) || !aligned(y_scale, 4)))) return JENGA_EINVAL;
+  if (!aligned(x, xs) || !aligned(residual, xs) || !aligned(total, xs) || (!packed && !aligned(y, xs)) || !aligned(weight, ps) ||
+      !aligned(rstd, 4))
+    return JENGA_EINVAL;
+  if ((why = rms_strides_ok(c->x_row, c->x_head, *c)) != JENGA_OK) return why;
+  if (residual && (why = rms_strides_ok(c->add_row, c->add_head, *c)) != JENGA_OK) return why;
+  if (total && (why = rms_strides_ok(c->sum_row, c->sum_head, *c)) != JENGA_OK) return why;
+  if (!packed && (why = rms_strides_ok(c->y_row, c->y_head, *c)) != JENGA_OK) return why;
+  if (c->rows == 0) return JENGA_OK;
+  const Layout4 from = rows_and_heads(x, c->x_row, c->x_head, c->rows, c->heads, c->cols, xs),
+                add = rows_and_heads(residual, c->add_row, c->add_head, c->rows, c->heads, c->cols, xs),
+                sum = rows_and_heads(total, c->sum_row, c->sum_head, c->rows, c->heads, c->cols, xs),
+                to = rows_and_heads(packed ? nullptr : y, c->y_row, c->y_head, c->rows, c->heads, c->cols, xs);
+  const int64_t stats = c->rows * c->heads * 4;
+  const Span read[1] = {{weight, 1, c->cols * ps, c->cols * ps}};
+  const Span written[3] = {{rstd, 1, stats, stats}, {packed ? y : nullptr, c->rows, y_bytes, y_bytes}, {y_scale, c->rows, scales, scales}};
+  if ((!packed && !distinct(to)) || (total && !distinct(sum))) return JENGA_EINVAL;
+  for (const Layout4* out : {&to, &sum}) {
+    for (const Layout4* in : {&from, &add})
+      if (touch(*out, *in) && !same_place(*out, *in)) return JENGA_EINVAL;
+    if (touch(*out, read[0])) return JENGA_EINVAL;
+  }
+  if (touch(to, sum)) return JENGA_EINVAL;
+  for (int i = 0; i < 3; ++i) {
+    for (const Layout4* t : {&from, &add, &sum, &to})
+      if (touch(*t, written[i])) return JENGA_EINVAL;
+    if (overlap(written[i], read[0])) return JENGA_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (overlap(written[i], written[j])) return JENGA_EINVAL;
+  }
+  return JENGA_OK;
+}
+
+int rms_grad_args_ok(const jenga_rms_config* c, const void* x, const void* dy, const void* weight, const float* rstd, const void* dtotal,
+                     const void* dx, const float* dweight, const void* workspace, size_t workspace_bytes) {
+  if (!c || !x || !dy || !rstd || !dx) return JENGA_EINVAL;
+  int why = rms_config_ok(*c);
+  if (why != JENGA_OK) return why;
+  if (c->y_type != c->x_type) return JENGA_EUNSUPPORTED;
+  const int64_t xs = type_size(c->x_type), ps = type_size(c->param_type);
+  if (!aligned(x, xs) || !aligned(dy, xs) || !aligned(dtotal, xs) || !aligned(dx, xs) || !aligned(weight, ps) || !aligned(rstd, 4) ||
+      !aligned(dweight, 4))
+    return JENGA_EINVAL;
+  if ((why = rms_strides_ok(c->x_row, c->x_head, *c)) != JENGA_OK) return why;
+  if (dtotal && (why = rms_strides_ok(c->add_row, c->add_head, *c)) != JENGA_OK) return why;
+  if ((why = rms_strides_ok(c->sum_row, c->sum_head, *c)) != JENGA_OK) return why;
+  if ((why = rms_strides_ok(c->y_row, c->y_head, *c)) != JENGA_OK) return why;
+  if (c->rows == 0) return JENGA_OK;
+  uint64_t need = 0;
+  if (dweight) {
+    if (!workspace || !aligned(workspace, 256)) return JENGA_EINVAL;
+    need = (uint64_t)RMS_PARTS * c->cols * 4;
+  }
+  const Layout4 from = rows_and_heads(x, c->x_row, c->x_head, c->rows, c->heads, c->cols, xs),
+                up = rows_and_heads(dy, c->y_row, c->y_head, c->rows, c->heads, c->cols, xs),
+                add = rows_and_heads(dtotal, c->add_row, c->add_head, c->rows, c->heads, c->cols, xs),
+                to = rows_and_heads(dx, c->sum_row, c->sum_head, c->rows, c->heads, c->cols, xs);
+  const int64_t stats = c->rows * c->heads * 4;
+  const Span params = {weight, 1, c->cols * ps, c->cols * ps}, r = {rstd, 1, stats, stats},
+             sums = {dweight, 1, (int64_t)c->cols * 4, (int64_t)c->cols * 4},
+             room = {need ? workspace : nullptr, 1, (int64_t)need, (int64_t)need};
+  if (!distinct(to) || touch(to, from) || touch(to, up) || (touch(to, add) && !same_place(to, add))) return JENGA_EINVAL;
+  for (const Layout4* t : {&from, &up, &add, &to})
+    if (touch(*t, sums) || touch(*t, room)) return JENGA_EINVAL;
+  if (touch(to, params) || touch(to, r)) return JENGA_EINVAL;
+  for (const Span* s : {&params, &r})
+    if (overlap(sums, *s) || overlap(room, *s)) return JENGA_EINVAL;
+  if (overlap(sums, room)) return JENGA_EINVAL;
+  return workspace_bytes < need ? JENGA_EWORKSPACE : JENGA_OK;
+}
+
+int quantize_mx_args_ok(const void* x, int64_t x_stride, int32_t x_type, int64_t rows, int32_t cols, const void* q, const uint8_t* scale) {
+  if (!x || !q || !scale || rows < 0 || cols < 1 || x_stride < cols) return JENGA_EINVAL;
+  if (!float_type(x_type) || !aligned(x, type_size(x_type)) || !aligned(q, 16) || !aligned(scale, 4)) return JENGA_EINVAL;
+  if (cols > MOST_COLS || rows > 1ll << 30 || x_stride > 1ll << 28) return JENGA_EUNSUPPORTED;
+  if (rows == 0) return JENGA_OK;
+  const int64_t size = type_size(x_type), blocks = ((int64_t)cols + 127) / 128;
+  const Span from = {x, rows, x_stride * size, cols * size}, to = {q, rows, blocks * 64, blocks * 64}, bytes = {scale, rows, blocks * 4, blocks * 4};
+  return overlap(from, to) || overlap(from, bytes) || overlap(to, bytes) ? JENGA_EINVAL : JENGA_OK;
+}
+
+int matmul_mx_args_ok(const jenga_matmul_config* c, const void* a, const uint8_t* a_scale, const void* b, const uint8_t* b_scale,
+                      const float* bias, const void* out) {
+  if (!c || !a || !a_scale || !b || !b_scale || !out) return JENGA_EINVAL;
+  if (c->m < 0 || c->n < 1 || c->k < 1 || c->k % 128 != 0 || c->out_stride < c->n || c->reserved != 0) return JENGA_EINVAL;
+  if (!float_type(c->out_type)) return JENGA_EINVAL;
+  const int64_t size = type_size(c->out_type);
+  if (!aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4) || !aligned(bias, 4) || !aligned(out, size))
+    return JENGA_EINVAL;
+  if (c->k > MOST_COLS || c->m > 1ll << 30 || c->n > 1 << 22 || c->out_stride > 1ll << 31) return JENGA_EUNSUPPORTED;
+  if ((c->m + 127) / 128 * (((int64_t)c->n + 127) / 128) > 1ll << 23) return JENGA_EUNSUPPORTED;
+  if (c->m == 0) return JENGA_OK;
+  const int64_t values = c->k / 2, scales = c->k / 32;
+  const Span to = {out, c->m, c->out_stride * size, c->n * size};
+  const Span in[5] = {{a, c->m, values, values}, {a_scale, c->m, scales, scales}, {b, c->n, values, values}, {b_scale, c->n, scales, scales},
+                      {bias, 1, (int64_t)c->n * 4, (int64_t)c->n * 4}};
+  for (const Span& s : in)
+    if (overlap(to, s)) return JENGA_EINVAL;
+  return JENGA_OK;
+}
+
+int dense_config_ok(const jenga_dense_config* c) {
+  if (!c || c->q_rows < 0 || c->kv_rows < 0 || c->sequences < 0 || c->heads < 1 || c->kv_heads < 1 || c->heads % c->kv_heads != 0 ||
+      c->reserved != 0)
+    return JENGA_EINVAL;
+  if ((c->type != JENGA_BF16 && c->type != JENGA_F16) || (c->flags & ~(uint32_t)JENGA_DENSE_CAUSAL) || !std::isnormal(c->scale * 1.4426950408889634f) || c->scale < 0.0f)
+    return JENGA_EINVAL;
+  if (c->head_dim < 1) return JENGA_EINVAL;
+  if ((c->head_dim != 64 && c->head_dim != 128) || c->sequences > 1 << 16 || c->heads > 1 << 12) return JENGA_EUNSUPPORTED;
+  const int64_t most = (1ll << 31) - 1;
+  if (c->q_rows > most || c->kv_rows > most || c->q_rows * (c->heads / c->kv_heads) > most) return JENGA_EUNSUPPORTED;
+  if (dense_shape(*c).items * c->kv_heads > 1 << 23) return JENGA_EUNSUPPORTED;   // workgroups of a launch
+  return JENGA_OK;
+}
+
+int dense_args_ok(const jenga_dense_config* c, const void* q, const void* k, const void* v, const int32_t* q_start,
+                  const int32_t* kv_start, const int32_t* kv_len, const void* out, const void* workspace, size_t workspace_bytes) {
+  const int why = dense_config_ok(c);
+  if (why != JENGA_OK) return why;
+  if (!q || !k || !v || !q_start || !kv_start || !out || !workspace) return JENGA_EINVAL;
+  if (!aligned(q, 2) || !aligned(k, 2) || !aligned(v, 2) || !aligned(out, 2) || !aligned(q_start, 4) || !aligned(kv_start, 4) ||
+      !aligned(kv_len, 4) || !aligned(workspace, 256))
+    return JENGA_EINVAL;
+  const struct { int64_t row, head, heads; } strides[4] = {{c->q_row, c->q_head, c->heads},
+                                                                 {c->k_row, c->k_head, c->kv_heads},
+                                                                 {c->v_row, c->v_head, c->kv_heads},
+                                                                 {c->out_row, c->out_head, c->heads}};
+  for (const auto& s : strides) {
+    if (s.row < 0 || s.head < 0) return JENGA_EINVAL;
+    if (s.row > 1 << 23 || s.head > MOST_STRIDE || (__int128)s.head * s.heads > (__int128)1 << 60) return JENGA_EUNSUPPORTED;
+  }
+  const uint64_t need = dense_shape(*c).workspace;
+  if (c->q_rows > 0) {
+    const Layout4 to = rows_and_heads(out, c->out_row, c->out_head, c->q_rows, c->heads, c->head_dim, 2),
+                  from = rows_and_heads(q, c->q_row, c->q_head, c->q_rows, c->heads, c->head_dim, 2);
+    const Layout4 keys = rows_and_heads(c->kv_rows ? k : nullptr, c->k_row, c->k_head, c->kv_rows, c->kv_heads, c->head_dim, 2),
+                  values = rows_and_heads(c->kv_rows ? v : nullptr, c->v_row, c->v_head, c->kv_rows, c->kv_heads, c->head_dim, 2);
+    if (!distinct(to) || (touch(to, from) && !same_place(to, from)) || touch(to, keys) || touch(to, values)) return JENGA_EINVAL;
+    const int64_t starts = ((int64_t)c->sequences + 1) * 4, lengths = (int64_t)c->sequences * 4;
+    const Span room = {workspace, 1, (int64_t)need, (int64_t)need};
+    for (const Span& s : {Span{q_start, 1, starts, starts}, Span{kv_start, 1, starts, starts}, Span{lengths ? kv_len : nullptr, 1, lengths, lengths}})
+      if (touch(to, s) || overlap(s, room)) return JENGA_EINVAL;
+    if (touch(to, room) || touch(from, room) || touch(keys, room) || touch(values, room)) return JENGA_EINVAL;
+  }
+  return workspace_bytes < need ? JENGA_EWORKSPACE : JENGA_OK;
+}
+
+DenseShape dense_shape(const jenga_dense_config& c) {
+  DenseShape s;
+  const int64_t group = c.heads / c.kv_heads, rows = c.q_rows * group;
+  s.rows = rows <= 32 * (int64_t)c.sequences ? 16 : 128;
+  s.workgroups = s.rows == 16 ? 512 : 768;
+  // each sequence ends with a tile that may not be full
+  s.tiles = rows == 0 ? 0 : rows / s.rows + c.sequences;
+  // full tiles that there are at least
+  const int64_t least = rows / s.rows;
+  s.may_split = least * c.kv_heads < s.workgroups;
+  // a tile of n steps makes ceil(n / chunk) parts, and all steps together workgroups / kv_heads chunks at most
+  const int64_t split = (s.workgroups + c.kv_heads - 1) / c.kv_heads;
+  s.split_tiles = s.may_split ? std::min<int64_t>(s.tiles, split) : 0;
+  s.items = s.may_split ? std::max<int64_t>(s.tiles, s.split_tiles + split) : s.tiles;
+  s.slots = s.may_split ? s.split_tiles + split : 0;
+  auto up = [](uint64_t bytes) { return (bytes + 255) / 256 * 256; };
+  s.bins_at = 256;
+  s.items_at = s.bins_at + up(((uint64_t)c.sequences + 1) * 4 * DENSE_LEVELS);
+  s.merge_at = s.items_at + up((uint64_t)s.items * sizeof(DenseItem));
+  s.stat_at = s.merge_at + up((uint64_t)s.split_tiles * sizeof(DenseMerge));
+  const uint64_t results = (uint64_t)s.slots * c.kv_heads * s.rows;
+  s.part_at = s.stat_at + up(results * 8);
+  s.workspace = s.part_at + up(results * c.head_dim * 4);
+  return s;
+}
+
 }  // namespace jenga
 
 extern "C" {
+
+int jenga_rms_norm_grad_workspace(const jenga_rms_config* c, uint64_t* bytes) {
+  if (!c || !bytes) return JENGA_EINVAL;
+  const int why = jenga::rms_config_ok(*c);
+  if (why != JENGA_OK) return why;
+  *bytes = (uint64_t)jenga::RMS_PARTS * c->cols * 4;
+  return JENGA_OK;
+}
+
+int jenga_dense_attn_workspace(const jenga_dense_config* c, uint64_t* bytes) {
+  if (!bytes) return JENGA_EINVAL;
+  const int why = jenga::dense_config_ok(c);
+  if (why != JENGA_OK) return why;
+  *bytes = jenga::dense_shape(*c).workspace;
+  return JENGA_OK;
+}
 
 int jenga_layer_norm_grad_workspace(const jenga_norm_config* c, uint64_t* bytes) {
   if (!c || !bytes) return JENGA_EINVAL;

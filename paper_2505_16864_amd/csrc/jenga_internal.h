@@ -197,6 +197,30 @@ struct MatmulTiles {
   int per_cu;               // workgroups on a compute unit
 };
 MatmulTiles matmul_tiles(int64_t m, int64_t n, bool float32);
+MatmulTiles matmul_mx_tiles(int64_t m, int64_t n);   // of 4-bit operands
+
+// Dense attention.  The rows of a sequence and of the heads that share keys are packed, row n is token n / group, head n % group, and cut
+// into tiles of `rows` rows.  Lengths are on the device, so a first kernel makes the list of work, DenseItems, of which the
+// host knows bounds.
+struct DenseItem {
+  int32_t q0, nq;        // the sequence: first row of q, rows
+  int32_t kv0, nk;       // first key, keys
+  int32_t row0;          // the tile: first packed row
+  int32_t begin, end;    // keys of this part
+  int32_t slot;          // of the partial result, -1: the part is the whole tile
+};
+struct DenseMerge {
+  int32_t q0, nq, row0, slot, parts, reserved;
+};
+constexpr int DENSE_LEVELS = 4;
+struct DenseShape {
+  int rows;                                        // of a tile
+  int64_t tiles, items, slots, split_tiles;        // at most, for each head of keys
+  int64_t workgroups;                              // that tiles are cut for
+  bool may_split;
+  uint64_t bins_at, items_at, merge_at, stat_at, part_at, workspace;   // bytes
+};
+DenseShape dense_shape(const jenga_dense_config& c);
 
 // Checks of arguments (jenga_host.cpp), all of a call's that need no device.  They return a jenga_status.
 int norm_args_ok(const jenga_norm_config* c, const void* x, const void* weight, const void* bias, const void* y, const uint8_t* y_scale,
@@ -208,6 +232,16 @@ int quantize_args_ok(const void* x, int64_t x_stride, int32_t x_type, int64_t ro
                      const uint8_t* scale);
 int matmul_args_ok(const jenga_matmul_config* c, const void* a, const uint8_t* a_scale, const void* b, const uint8_t* b_scale,
                    const float* bias, const void* out);
+int rms_args_ok(const jenga_rms_config* c, const void* x, const void* residual, const void* weight, const void* total, const void* y,
+                const uint8_t* y_scale, const float* rstd);
+int rms_grad_args_ok(const jenga_rms_config* c, const void* x, const void* dy, const void* weight, const float* rstd, const void* dtotal,
+                     const void* dx, const float* dweight, const void* workspace, size_t workspace_bytes);
+int quantize_mx_args_ok(const void* x, int64_t x_stride, int32_t x_type, int64_t rows, int32_t cols, const void* q, const uint8_t* scale);
+int matmul_mx_args_ok(const jenga_matmul_config* c, const void* a, const uint8_t* a_scale, const void* b, const uint8_t* b_scale,
+                      const float* bias, const void* out);
+int dense_config_ok(const jenga_dense_config* c);
+int dense_args_ok(const jenga_dense_config* c, const void* q, const void* k, const void* v, const int32_t* q_start,
+                  const int32_t* kv_start, const int32_t* kv_len, const void* out, const void* workspace, size_t workspace_bytes);
 int rotary_config_ok(const jenga_rotary_config* c);
 int rotary_args_ok(const jenga_rotary_config* c, const jenga_plan* plan, const int32_t* cells, const float* table,
                    const jenga_rotary_tensor* tensors, int32_t count, int64_t batch, int64_t tokens);
