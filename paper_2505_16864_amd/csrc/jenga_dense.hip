@@ -7,8 +7,9 @@
 // products S^T = K Q^T and O^T = V^T P^T keep a row in one lane of every accumulator, and the accumulators of S^T are the operand of
 // the second product as they are.
 //
-// Three launches: the list of work from the lengths, which are on the device; the tiles, of which long ones are cut along their keys where
-// there are few; and, if some may be, the joining of their parts in the order of the keys.
+// Lengths are on the device.  A workgroup finds its tile from them; where there are more than 64 sequences, which is what a wavefront looks at
+// in one go, a first launch makes a list instead.  Where there are few tiles, long ones are cut along their keys, and a second launch joins the
+// parts in the order of the keys.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -38,9 +39,9 @@ struct DenseArgs {
   uint32_t by_group, group_shift;
   int32_t causal;
   float scale_log2e;
-  int32_t tile, keys, max_tiles, workgroups, may_split;   // keys: of a step
-  int32_t *counts, *bins;   // items and merges; tiles of the sequences in front of each
-  DenseItem* items;
+  int32_t tile, keys, max_tiles, max_slots, workgroups, may_split;   // keys: of a step
+  int32_t *counts, *bins;   // of a list: items and merges; tiles of the sequences in front of each
+  DenseItem* items;         // or NULL
   DenseMerge* merges;
   float *stat, *part;       // [slot][kv_heads][tile][2]: reference, sum; [slot][kv_heads][tile][D]
 };
@@ -101,6 +102,32 @@ __device__ __forceinline__ bool not_finite(uint32_t w) {
   return ((v - 0x00010001u) & ~v & 0x80008000u) != 0;
 }
 
+// The finite ones of two values, 0 for the others.
+template <typename T>
+__device__ __forceinline__ uint32_t finite_part(uint32_t w) {
+  const uint32_t e = w & Type<T>::EXPONENT;
+  return ((e & 0xFFFFu) == (Type<T>::EXPONENT & 0xFFFFu) ? 0u : w & 0xFFFFu) | ((e >> 16) == (Type<T>::EXPONENT >> 16) ? 0u : w & 0xFFFF0000u);
+}
+// A value that is not finite, 0 for others.
+template <typename T>
+__device__ __forceinline__ float rest_of(T v) {
+  const float f = (float)v;
+  return fabsf(f) < __builtin_inff() ? 0.f : f;
+}
+// Values that are not finite, of keys that some rows of a tile do not see: a probability of 0 is not enough there.  They are taken out of LDS,
+// 16 bytes a lane, by the wavefront that has copied them; rows that see them get them behind the loop.  Returns whether there were any.
+template <typename T>
+__device__ __forceinline__ bool take_out(uint32_t lds) {
+  u32x4 w = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)lds;
+  const bool found = not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
+  if (found) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = finite_part<T>(w[i]);
+    *(__attribute__((address_space(3))) u32x4*)(uintptr_t)lds = w;
+  }
+  return found;
+}
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Four rows x 16 channels of 16 bits, a row by four lanes of 8 bytes, to the 16 lanes of a group: lane i gets channel i, row 0 first.
@@ -140,6 +167,109 @@ __device__ __forceinline__ int keys_of_tile(const DenseArgs& a, const Lengths& n
   return max(0, min(n.nk, (int)min((int64_t)last + 1 + n.nk - n.nq, (int64_t)n.nk)));
 }
 
+__device__ __forceinline__ int tiles_of(const DenseArgs& a, const Lengths& n) {
+  return (int)(((int64_t)n.nq * a.group + a.tile - 1) / a.tile);
+}
+__device__ __forceinline__ int steps_of(const DenseArgs& a, int keys) { return (keys + a.keys - 1) / a.keys; }
+// Tile t of a sequence; the last ones, which see the most keys, come first.
+__device__ __forceinline__ DenseItem item_of(const DenseArgs& a, const Lengths& n, int tiles, int t) {
+  DenseItem item = {n.q0, n.nq, n.kv0, n.nk, (a.causal ? tiles - 1 - t : t) * a.tile, 0, 0, -1};
+  item.end = keys_of_tile(a, n, item.row0);
+  return item;
+}
+// Part `part` of `parts` of an item, in whole steps.
+__device__ __forceinline__ void take_part(const DenseArgs& a, DenseItem* item, int part, int parts, int slot) {
+  if (parts == 1) return;
+  const int64_t steps = steps_of(a, item->end);
+  item->begin = (int)(steps * part / parts) * a.keys;
+  item->end = min(item->end, (int)(steps * (part + 1) / parts) * a.keys);
+  item->slot = slot;
+}
+// Steps of a part at least.  A part costs its start, its results and their joining: shorter ones than 256 keys lose.
+__device__ __forceinline__ int least_steps(const DenseArgs& a) { return 256 / a.keys; }
+
+// Sum over this lane and those in front of it.
+__device__ __forceinline__ int lanes_scan(int v) {
+  auto moved = [](int x, auto ctrl, auto mask) { return __builtin_amdgcn_update_dpp(0, x, decltype(ctrl)::value, decltype(mask)::value, 0xF, false); };
+  using std::integral_constant;
+  v += moved(v, integral_constant<int, 0x111>{}, integral_constant<int, 0xF>{});   // row_shr 1, 2, 4, 8
+  v += moved(v, integral_constant<int, 0x112>{}, integral_constant<int, 0xF>{});
+  v += moved(v, integral_constant<int, 0x114>{}, integral_constant<int, 0xF>{});
+  v += moved(v, integral_constant<int, 0x118>{}, integral_constant<int, 0xF>{});
+  v += moved(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});   // row_bcast 15 and 31
+  v += moved(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});
+  return v;
+}
+
+// 64 sequences at most, one a lane: what the call's work is.  A tile is cut into ceil(steps / chunk) parts, and all tiles of a sequence have
+// as many places as the longest of them has parts.
+struct Work {
+  Lengths n;
+  int tiles, chunk, parts;   // chunk 0: nothing is cut
+  int tiles_before, items_before;   // with this lane's own
+};
+__device__ __forceinline__ Work work_of_lane(const DenseArgs& a) {
+  const int lane = threadIdx.x & 63;
+  Work w = {};
+  if (lane < a.sequences) w.n = lengths_of(a, lane), w.tiles = tiles_of(a, w.n);
+  w.tiles_before = lanes_scan(w.tiles);
+  w.parts = 1;
+  w.items_before = w.tiles_before;
+  const int all = __builtin_amdgcn_readlane(w.tiles_before, 63);
+  if (!a.may_split || all < 0 || (int64_t)all * a.kv_heads >= a.workgroups) return w;
+  float steps = 0.f;   // of all tiles of the sequence: from the first one's to the last one's
+  if (w.tiles > 0) steps = 0.5f * (float)w.tiles * ((float)steps_of(a, keys_of_tile(a, w.n, 0)) + (float)steps_of(a, w.n.nk));
+  const float total = wave_sum_f32(steps) * (float)a.kv_heads;
+  w.chunk = max((int)ceilf(total / (float)a.workgroups), least_steps(a));
+  w.parts = max(1, (steps_of(a, w.n.nk) + w.chunk - 1) / w.chunk);
+  w.items_before = lanes_scan(w.tiles * w.parts);
+  return w;
+}
+__device__ __forceinline__ Lengths lengths_from(const Lengths& n, int lane) {
+  return {__builtin_amdgcn_readlane(n.q0, lane), __builtin_amdgcn_readlane(n.nq, lane), __builtin_amdgcn_readlane(n.kv0, lane),
+          __builtin_amdgcn_readlane(n.nk, lane)};
+}
+__device__ __forceinline__ int parts_of(const DenseArgs& a, int chunk, int keys) {
+  return chunk == 0 ? 1 : max(1, (steps_of(a, keys) + chunk - 1) / chunk);
+}
+// Item `index` of the call, the same for all lanes; false: there is none.  Slots past the last one: starts that do not ascend.
+__device__ __forceinline__ bool find_item(const DenseArgs& a, int index, DenseItem* item) {
+  if (a.items) {
+    if (index >= a.counts[0]) return false;
+    *item = a.items[index];
+    return true;
+  }
+  const Work w = work_of_lane(a);
+  const uint64_t behind = __ballot(w.items_before > index);
+  if (behind == 0) return false;
+  const int s = __builtin_ctzll(behind), tiles = __builtin_amdgcn_readlane(w.tiles, s), places = __builtin_amdgcn_readlane(w.parts, s);
+  const int chunk = __builtin_amdgcn_readfirstlane(w.chunk), first = __builtin_amdgcn_readlane(w.items_before, s) - tiles * places;
+  const int tile = (index - first) / places, part = index - first - tile * places;
+  *item = item_of(a, lengths_from(w.n, s), tiles, tile);
+  const int parts = parts_of(a, chunk, item->end);
+  if (part >= parts || (parts > 1 && index >= a.max_slots)) return false;
+  take_part(a, item, part, parts, index);
+  return true;
+}
+// Tile `index` of the call, if it was cut.
+__device__ __forceinline__ bool find_merge(const DenseArgs& a, int index, DenseMerge* merge) {
+  if (a.items) {
+    if (index >= a.counts[1]) return false;
+    *merge = a.merges[index];
+    return true;
+  }
+  const Work w = work_of_lane(a);
+  const uint64_t behind = __ballot(w.tiles_before > index);
+  const int chunk = __builtin_amdgcn_readfirstlane(w.chunk);
+  if (behind == 0 || chunk == 0) return false;
+  const int s = __builtin_ctzll(behind), tiles = __builtin_amdgcn_readlane(w.tiles, s), places = __builtin_amdgcn_readlane(w.parts, s);
+  const int tile = index - (__builtin_amdgcn_readlane(w.tiles_before, s) - tiles);
+  const DenseItem item = item_of(a, lengths_from(w.n, s), tiles, tile);
+  *merge = {item.q0, item.nq, item.row0, __builtin_amdgcn_readlane(w.items_before, s) - tiles * places + tile * places,
+            parts_of(a, chunk, item.end), 0};
+  return merge->parts > 1 && merge->slot >= 0 && merge->slot + merge->parts <= a.max_slots;
+}
+
 // Sum over the threads in front; *total: over all of them.
 __device__ __forceinline__ int64_t scan(int64_t v, int64_t* room, int64_t* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -175,8 +305,8 @@ __global__ __launch_bounds__(1024) void dense_plan_kernel(DenseArgs a) {
   constexpr int IN_LDS = 4096;
   __shared__ int64_t room[16];
   __shared__ int32_t bins_here[IN_LDS];
-  __shared__ int32_t of_tile[1024][3];   // steps, first item, first slot
-  __shared__ int32_t first_item[1025];
+  __shared__ int32_t of_tile[1024][2];   // parts, first slot
+  __shared__ int32_t first_item[1024];
   const int tid = threadIdx.x;
   int32_t* bins = a.sequences <= IN_LDS ? bins_here : a.bins;
   int64_t tiles = 0, total;
@@ -189,25 +319,14 @@ __global__ __launch_bounds__(1024) void dense_plan_kernel(DenseArgs a) {
     tiles += total;
   }
   __syncthreads();
-  auto tile_at_index = [&](int j, DenseItem* item) {
+  auto tile_at_index = [&](int j) {
     const int s = last_below(bins, a.sequences, j);
     const Lengths n = lengths_of(a, s);
-    item->q0 = n.q0;
-    item->nq = n.nq;
-    item->kv0 = n.kv0;
-    item->nk = n.nk;
-    item->row0 = (j - bins[s]) * a.tile;
-    item->begin = 0;
-    item->end = keys_of_tile(a, n, item->row0);
-    item->slot = -1;
+    return item_of(a, n, tiles_of(a, n), j - bins[s]);
   };
   const int n_tiles = (int)min(tiles, (int64_t)a.max_tiles);   // more only where starts do not ascend
   if (!a.may_split || tiles * a.kv_heads >= a.workgroups) {
-    for (int j = tid; j < n_tiles; j += 1024) {
-      DenseItem item;
-      tile_at_index(j, &item);
-      a.items[j] = item;
-    }
+    for (int j = tid; j < n_tiles; j += 1024) a.items[j] = tile_at_index(j);
     if (tid == 0) a.counts[0] = n_tiles, a.counts[1] = 0;
     return;
   }
@@ -215,33 +334,28 @@ __global__ __launch_bounds__(1024) void dense_plan_kernel(DenseArgs a) {
   DenseItem mine = {};
   int steps = 0;
   if (tid < n_tiles) {
-    tile_at_index(tid, &mine);
-    steps = (mine.end + a.keys - 1) / a.keys;
+    mine = tile_at_index(tid);
+    steps = steps_of(a, mine.end);
   }
   int64_t all;
   scan(steps, room, &all);
-  const int chunk = (int)max((all * a.kv_heads + a.workgroups - 1) / a.workgroups, (int64_t)1);
+  const int chunk = (int)max((all * a.kv_heads + a.workgroups - 1) / a.workgroups, (int64_t)least_steps(a));
   const int parts = tid < n_tiles ? max((steps + chunk - 1) / chunk, 1) : 0;
   int64_t n_items, n_slots, n_merges;
   const int item0 = (int)scan(parts, room, &n_items);
   const int slot0 = (int)scan(parts > 1 ? parts : 0, room, &n_slots);
   const int merge0 = (int)scan(parts > 1 ? 1 : 0, room, &n_merges);
   if (tid < n_tiles) {
-    of_tile[tid][0] = steps;
-    of_tile[tid][1] = parts;
-    of_tile[tid][2] = parts > 1 ? slot0 : -1;
+    of_tile[tid][0] = parts;
+    of_tile[tid][1] = slot0;
     first_item[tid] = item0;
     if (parts > 1) a.merges[merge0] = {mine.q0, mine.nq, mine.row0, slot0, parts, 0};
   }
   __syncthreads();
   for (int i = tid; i < n_items; i += 1024) {
-    const int j = last_below(first_item, n_tiles, i);
-    DenseItem item;
-    tile_at_index(j, &item);
-    const int part = i - first_item[j], n = of_tile[j][1], st = of_tile[j][0];
-    item.begin = (int)((int64_t)st * part / n) * a.keys;
-    item.end = min(item.end, (int)((int64_t)st * (part + 1) / n) * a.keys);
-    item.slot = of_tile[j][2] < 0 ? -1 : of_tile[j][2] + part;
+    const int j = last_below(first_item, n_tiles, i), part = i - first_item[j];
+    DenseItem item = tile_at_index(j);
+    take_part(a, &item, part, of_tile[j][0], of_tile[j][1] + part);
     a.items[i] = item;
   }
   if (tid == 0) a.counts[0] = (int)n_items, a.counts[1] = (int)n_merges;
@@ -278,15 +392,15 @@ __device__ __forceinline__ u32x4 keys_of_step(const uint16_t* base, int64_t row_
 // undefined sends the step down the exact path: logits again, the row's maximum, what has been added up rescaled, probabilities <= 1.  The first
 // step of a row starts there, so the reference never exceeds the largest logit seen and the largest term is never lost to underflow.
 template <typename T, int D, bool ALIGNED>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dense_tiles_kernel(DenseArgs a) {
+__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(DenseArgs a) {
   typedef typename Type<T>::eight eight;
   constexpr int KEYS = 64, KS = D / 16, DT = D / 32, MH = KEYS / 32, PH = KEYS / 16, CH = D / 8;
   constexpr int CHUNKS = KEYS * CH, COPIES = CHUNKS / 256, ROWS_PER_COPY = 256 / CH;
   __shared__ __attribute__((aligned(256))) u32x4 Ks[CHUNKS];
   __shared__ __attribute__((aligned(256))) u32x4 Vs[CHUNKS];
   const int index = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - index * a.kv_heads;
-  if (index >= a.counts[0]) return;
-  const DenseItem it = a.items[index];
+  DenseItem it;
+  if (!find_item(a, index, &it)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hl = lane >> 5, ql = lane & 31;
   int row = it.row0 + 32 * wave + ql;
   Row r = row_at(a, it, kv_head, row);
@@ -331,7 +445,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dense_tiles_kernel(Dens
   auto landed = []() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); };
 
   float m_run = r.limit > it.begin ? -__builtin_inff() : 0.f, l_run = 0.f;   // 0: a row that sees none of these keys
-  bool unset = true;
+  bool unset = true, taken = false;
   f32x16 O[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) O[dt] = 0.f;
@@ -408,6 +522,10 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dense_tiles_kernel(Dens
     }
     l_run += sum;
     landed();
+    if (masked && a.causal) {
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c) taken |= take_out<T>(vs_wave + c * 4096 + lane * 16);
+    }
     __syncthreads();   // V is in LDS; every wavefront has read K
     if (key + KEYS < it.end) copy(k0, a.k_row, k_from, Ks, ks_wave, key + KEYS);
     auto v_fragment = [&](int dt, int p) {
@@ -415,39 +533,18 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void dense_tiles_kernel(Dens
       const u32x2 lo = columns(at), hi = columns(at + 16 * D);
       return (u32x4){lo[0], lo[1], hi[0], hi[1]};
     };
-    // Keys that some rows do not see have probability 0 there, which is not enough where their values are not finite.
-    bool careful = false;
-    if (masked && a.causal) {
-      uint32_t found = 0;
-#pragma unroll 4
-      for (int i = lane; i < CHUNKS; i += 64) {
-        const u32x4 w = piece16(lds_address(Vs) + i * 16);
-        found |= not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
-      }
-      careful = __ballot(found != 0) != 0;
-    }
-    if (!careful) {
 #pragma unroll
-      for (int p = 0; p < PH; ++p)
+    for (int p = 0; p < PH; ++p)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul32(__builtin_bit_cast(eight, v_fragment(dt, p)), pb[p], O[dt]);
-    } else {   // a key at a time, and only for the rows that see it
+      for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul32(__builtin_bit_cast(eight, v_fragment(dt, p)), pb[p], O[dt]);
+  }
+  if (a.causal && __syncthreads_or(taken)) {   // what was taken out, to the rows that see it: it makes of a sum what it is itself
+    for (int key = it.begin + max(all_see - it.begin, 0) / KEYS * KEYS; key < min(it.end, r.limit); ++key) {
+      const T* v = (const T*)v0 + (int64_t)key * a.v_row + 4 * hl;
 #pragma unroll
-      for (int p = 0; p < PH; ++p)
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const u32x4 v = v_fragment(dt, p);
-#pragma unroll 1
-          for (int e = 0; e < 16; ++e) {
-            const int i = e & 7, half = e >> 3;
-            u32x4 one = 0u;
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-              if (w == i >> 1 && half == hl) one[w] = v[w] & (i & 1 ? 0xFFFF0000u : 0xFFFFu);
-            const f32x16 with = Type<T>::mul32(__builtin_bit_cast(eight, one), pb[p], O[dt]);
-            if (key + 16 * p + 8 * (i >> 2) + 4 * half + (i & 3) < r.limit) O[dt] = with;
-          }
-        }
+        for (int e = 0; e < 16; ++e) O[dt][e] += rest_of(v[32 * dt + 8 * (e / 4) + e % 4]);
     }
   }
 
@@ -493,8 +590,8 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
   __shared__ float stats[4][16][2];
   static_assert(ROOM >= 16 * D * 4, "");
   const int index = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - index * a.kv_heads;
-  if (index >= a.counts[0]) return;
-  const DenseItem it = a.items[index];
+  DenseItem it;
+  if (!find_item(a, index, &it)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, i16 = lane & 15;
   const Row r = row_at(a, it, kv_head, it.row0 + i16);
   const int first_token = (int)token_of(a, (uint32_t)it.row0);
@@ -534,7 +631,7 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
     copy(v0, a.v_row, v_swizzle, key, lds + stage * 2 * BYTES + BYTES);
   };
   float m_run = r.limit > it.begin ? -__builtin_inff() : 0.f, l_run = 0.f;
-  bool unset = true;
+  bool unset = true, taken = false;
   f32x4 O[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) O[dt] = 0.f;
@@ -542,7 +639,8 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
   const int v_row = 4 * g + ((lane >> 2) & 3);
   const uint32_t v_lane = BYTES + v_row * (2 * D) + (((lane >> 1) & 1) ^ v_swizzle(v_row)) * 16 + (lane & 1) * 8;
 
-  int key = it.begin + KEYS * wave, stage = 0;
+  const int first_key = it.begin + KEYS * wave;
+  int key = first_key, stage = 0;
   if (key < it.end) {
     copy_step(key, 0);
     copy_step(key + 4 * KEYS, 1);
@@ -551,6 +649,10 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(ALIGNED ? 2 * COPIES : 0) : "memory");
     const uint32_t at = lds + stage * 2 * BYTES;
     const bool masked = key + KEYS > all_see;
+    if (masked && a.causal) {
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c) taken |= take_out<T>(at + BYTES + c * 1024 + lane * 16);
+    }
     f32x4 S[2] = {};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
@@ -608,39 +710,25 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
       const u32x2 lo = columns(from), hi = columns(from + 32 * D);
       return (u32x4){lo[0], lo[1], hi[0], hi[1]};
     };
-    bool careful = false;
-    if (masked && a.causal) {
-      uint32_t found = 0;
 #pragma unroll
-      for (int i = 0; i < COPIES; ++i) {
-        const u32x4 w = piece16(at + BYTES + i * 1024 + lane * 16);
-        found |= not_finite<T>(w[0]) | not_finite<T>(w[1]) | not_finite<T>(w[2]) | not_finite<T>(w[3]);
-      }
-      careful = __ballot(found != 0) != 0;
-    }
-    if (!careful) {
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul16(__builtin_bit_cast(eight, v_fragment(dt)), pb, O[dt]);
-    } else {   // a key at a time, and only for the rows that see it
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const u32x4 v = v_fragment(dt);
-#pragma unroll 1
-        for (int e = 0; e < 32; ++e) {
-          const int i = e & 7, of = e >> 3;
-          u32x4 one = 0u;
-#pragma unroll
-          for (int w = 0; w < 4; ++w)
-            if (w == i >> 1 && of == g) one[w] = v[w] & (i & 1 ? 0xFFFF0000u : 0xFFFFu);
-          const f32x4 with = Type<T>::mul16(__builtin_bit_cast(eight, one), pb, O[dt]);
-          if (key + 16 * (i >> 2) + 4 * of + (i & 3) < r.limit) O[dt] = with;
-        }
-      }
-    }
+    for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul16(__builtin_bit_cast(eight, v_fragment(dt)), pb, O[dt]);
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // this stage has been read
     copy_step(key + 8 * KEYS, stage);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");   // nothing is on its way into LDS
+
+  if (a.causal && __ballot(taken) != 0) {   // what was taken out, to the rows that see it: it makes of a sum what it is itself
+    for (int step = first_key; step < it.end; step += 4 * KEYS) {
+      if (step + KEYS <= all_see) continue;
+      for (int j = step; j < min(min(step + KEYS, it.end), r.limit); ++j) {
+        const T* v = (const T*)v0 + (int64_t)j * a.v_row + 4 * g;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) O[dt][e] += rest_of(v[16 * dt + e]);
+      }
+    }
+  }
 
   // the four wavefronts' results
   l_run += __shfl_xor(l_run, 16);
@@ -682,47 +770,61 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
 
 // ---- joining
 
-// A workgroup a tile that was cut: the parts in their order, relative to the largest reference.
+// A wavefront a row of a tile that was cut: a lane looks at a part's reference and sum, 64 of them at a time, then groups of lanes with four
+// channels each take a part each.
 template <typename T, int D, int TILE>
 __global__ __launch_bounds__(256) void dense_merge_kernel(DenseArgs a) {
-  __shared__ float tops[TILE], invs[TILE];
-  const int index = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - index * a.kv_heads;
-  if (index >= a.counts[1]) return;
-  const DenseMerge it = a.merges[index];
-  const int64_t first = ((int64_t)it.slot * a.kv_heads + kv_head) * TILE, step = (int64_t)a.kv_heads * TILE;
-  const int rows = min(TILE, it.nq * a.group - it.row0);
-  if ((int)threadIdx.x < rows) {
-    const float* s = a.stat + 2 * (first + threadIdx.x);
-    float top = -__builtin_inff(), l = 0.f;
-    for (int p = 0; p < it.parts; ++p)
-      if (s[2 * step * p + 1] != 0.f) top = fmaxf(top, s[2 * step * p]);
-    for (int p = 0; p < it.parts; ++p)
-      if (s[2 * step * p + 1] != 0.f) l = fmaf(s[2 * step * p + 1], exp2_of(s[2 * step * p] - top), l);
-    tops[threadIdx.x] = top;
-    invs[threadIdx.x] = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < rows * (D / 4); i += 256) {
-    const int row = i / (D / 4), c = i % (D / 4) * 4;
-    f32x4 o = 0.f;
-    for (int p = 0; p < it.parts; ++p) {
-      const int64_t n = first + step * p + row;
-      if (a.stat[2 * n + 1] != 0.f) o += *(const f32x4*)(a.part + n * D + c) * exp2_of(a.stat[2 * n] - tops[row]);
+  constexpr int LANES = D / 4, GROUPS = 64 / LANES, BLOCKS = TILE / 4;
+  const int block = blockIdx.x % BLOCKS, of = blockIdx.x / BLOCKS, index = of / a.kv_heads, kv_head = of - index * a.kv_heads;
+  DenseMerge it;
+  if (!find_merge(a, index, &it)) return;
+  const int lane = threadIdx.x & 63, row = 4 * block + (threadIdx.x >> 6), group = lane / LANES, c = lane % LANES * 4;
+  const uint32_t t = token_of(a, (uint32_t)(it.row0 + row));
+  if ((int)t >= it.nq) return;
+  const int64_t first = ((int64_t)it.slot * a.kv_heads + kv_head) * TILE + row, step = (int64_t)a.kv_heads * TILE;
+  float top = -__builtin_inff(), l = 0.f;
+  f32x4 o = 0.f;
+  for (int p0 = 0; p0 < it.parts; p0 += 64) {
+    float m = 0.f, sum = 0.f;
+    if (p0 + lane < it.parts) {
+      const float2 s = *(const float2*)(a.stat + 2 * (first + step * (p0 + lane)));
+      m = s.x;
+      sum = s.y;
     }
-    const uint32_t t = token_of(a, (uint32_t)(it.row0 + row));
-    const int head = kv_head * a.group + it.row0 + row - (int)t * a.group;
-    T* out = (T*)a.out + ((int64_t)it.q0 + t) * a.out_row + (int64_t)head * a.out_head + c;
+    float top_here = sum != 0.f ? m : -__builtin_inff();   // NaN is not 0
 #pragma unroll
-    for (int e = 0; e < 4; ++e) out[e] = (T)(o[e] * invs[row]);
+    for (int d = 1; d < 64; d <<= 1) top_here = fmaxf(top_here, __shfl_xor(top_here, d));
+    const float top_new = fmaxf(top, top_here), alpha = top_new == top ? 1.0f : exp2_of(top - top_new);
+    const float weight = sum != 0.f ? exp2_of(m - top_new) : 0.f;
+    top = top_new;
+    l = l * alpha + wave_sum_f32(sum * weight);
+    o *= alpha;
+    const int n = min(64, it.parts - p0);
+#pragma unroll 4
+    for (int p = group; p < n; p += GROUPS) {
+      const float w = __shfl(weight, p);
+      const f32x4 part = *(const f32x4*)(a.part + (first + step * (p0 + p)) * D + c);
+      if (w != 0.f) o += part * w;
+    }
   }
+#pragma unroll
+  for (int d = LANES; d < 64; d <<= 1)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
+  if (group != 0) return;
+  const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+  const int head = kv_head * a.group + it.row0 + row - (int)t * a.group;
+  T* out = (T*)a.out + ((int64_t)it.q0 + t) * a.out_row + (int64_t)head * a.out_head + c;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[e] = (T)(o[e] * inv);
 }
 
 int status() { return hipGetLastError() == hipSuccess ? JENGA_OK : JENGA_EHIP; }
 
 template <typename T, int D, bool ALIGNED>
 int run(const DenseArgs& a, const DenseShape& s, hipStream_t st) {
-  const unsigned grid = (unsigned)(s.items * a.kv_heads), merges = (unsigned)(s.split_tiles * a.kv_heads);
-  dense_plan_kernel<<<1, 1024, 0, st>>>(a);
+  const unsigned grid = (unsigned)(s.items * a.kv_heads), merges = (unsigned)(s.split_tiles * a.kv_heads * (s.rows / 4));
+  if (a.items) dense_plan_kernel<<<1, 1024, 0, st>>>(a);
   if (s.rows == 16) {
     dense_rows_kernel<T, D, ALIGNED><<<grid, 256, 0, st>>>(a);
     if (s.may_split) dense_merge_kernel<T, D, 16><<<merges, 256, 0, st>>>(a);
@@ -775,12 +877,13 @@ int jenga_dense_attn(const jenga_dense_config* cfg, const void* q, const void* k
   a.tile = s.rows;
   a.keys = s.rows == 16 ? 128 : 64;
   a.max_tiles = (int32_t)s.tiles;
+  a.max_slots = (int32_t)s.slots;
   a.workgroups = (int32_t)s.workgroups;
   a.may_split = s.may_split;
   uint8_t* ws = (uint8_t*)workspace;
   a.counts = (int32_t*)ws;
   a.bins = (int32_t*)(ws + s.bins_at);
-  a.items = (DenseItem*)(ws + s.items_at);
+  a.items = s.listed ? (DenseItem*)(ws + s.items_at) : nullptr;
   a.merges = (DenseMerge*)(ws + s.merge_at);
   a.stat = (float*)(ws + s.stat_at);
   a.part = (float*)(ws + s.part_at);

@@ -590,14 +590,16 @@ DenseShape dense_shape(const jenga_dense_config& c) {
   // full tiles that there are at least
   const int64_t least = rows / s.rows;
   s.may_split = least * c.kv_heads < s.workgroups;
-  // a tile of n steps makes ceil(n / chunk) parts, and all steps together workgroups / kv_heads chunks at most
-  const int64_t split = (s.workgroups + c.kv_heads - 1) / c.kv_heads;
+  s.listed = c.sequences > 64;
+  // A tile of n steps makes ceil(n / chunk) parts, and the steps of all tiles are workgroups / kv_heads chunks at most.  Without a list the tiles of a
+  // sequence have as many places as the longest has parts, and their steps are taken as half of that at least; sums are float32 there.
+  const int64_t split = (s.workgroups + c.kv_heads - 1) / c.kv_heads, chunks = s.listed ? split : 2 * split + 16;
   s.split_tiles = s.may_split ? std::min<int64_t>(s.tiles, split) : 0;
-  s.items = s.may_split ? std::max<int64_t>(s.tiles, s.split_tiles + split) : s.tiles;
-  s.slots = s.may_split ? s.split_tiles + split : 0;
+  s.slots = s.may_split ? s.split_tiles + chunks : 0;
+  s.items = std::max<int64_t>(s.tiles, s.slots);
   auto up = [](uint64_t bytes) { return (bytes + 255) / 256 * 256; };
   s.bins_at = 256;
-  s.items_at = s.bins_at + up(((uint64_t)c.sequences + 1) * 4 * DENSE_LEVELS);
+  s.items_at = s.bins_at + up(((uint64_t)c.sequences + 1) * 4);
   s.merge_at = s.items_at + up((uint64_t)s.items * sizeof(DenseItem));
   s.stat_at = s.merge_at + up((uint64_t)s.split_tiles * sizeof(DenseMerge));
   const uint64_t results = (uint64_t)s.slots * c.kv_heads * s.rows;

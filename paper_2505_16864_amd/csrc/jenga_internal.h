@@ -200,8 +200,7 @@ MatmulTiles matmul_tiles(int64_t m, int64_t n, bool float32);
 MatmulTiles matmul_mx_tiles(int64_t m, int64_t n);   // of 4-bit operands
 
 // Dense attention.  The rows of a sequence and of the heads that share keys are packed, row n is token n / group, head n % group, and cut
-// into tiles of `rows` rows.  Lengths are on the device, so a first kernel makes the list of work, DenseItems, of which the
-// host knows bounds.
+// into tiles of `rows` rows.  Lengths are on the device; the host knows bounds of what there is to do.
 struct DenseItem {
   int32_t q0, nq;        // the sequence: first row of q, rows
   int32_t kv0, nk;       // first key, keys
@@ -212,12 +211,11 @@ struct DenseItem {
 struct DenseMerge {
   int32_t q0, nq, row0, slot, parts, reserved;
 };
-constexpr int DENSE_LEVELS = 4;
 struct DenseShape {
   int rows;                                        // of a tile
   int64_t tiles, items, slots, split_tiles;        // at most, for each head of keys
   int64_t workgroups;                              // that tiles are cut for
-  bool may_split;
+  bool may_split, listed;                          // listed: a first launch makes a list of the work
   uint64_t bins_at, items_at, merge_at, stat_at, part_at, workspace;   // bytes
 };
 DenseShape dense_shape(const jenga_dense_config& c);
