@@ -43,7 +43,7 @@ struct DenseArgs {
   int32_t *counts, *bins;   // of a list: items and merges; tiles of the sequences in front of each
   DenseItem* items;         // or NULL
   DenseMerge* merges;
-  float *stat, *part;       // [slot][kv_heads][tile][2]: reference, sum; [slot][kv_heads][tile][D]
+  float *stat, *part;       // [slot][kv_heads][tile][2]: reference, sum; [slot][kv_heads][tile][D], 128 rows in the order of the accumulators
 };
 
 // ---- the two types
@@ -130,6 +130,9 @@ __device__ __forceinline__ bool take_out(uint32_t lds) {
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// The reference that a part's results are joined by: of an undefined sum the largest, so that it is not lost beside others.
+__device__ __forceinline__ float reference_of(float m, float l) { return l == l ? m : __builtin_inff(); }
+
 // Four rows x 16 channels of 16 bits, a row by four lanes of 8 bytes, to the 16 lanes of a group: lane i gets channel i, row 0 first.
 __device__ __forceinline__ u32x2 columns(uint32_t lds) {
   u32x2 r = {};
@@ -187,6 +190,26 @@ __device__ __forceinline__ void take_part(const DenseArgs& a, DenseItem* item, i
 }
 // Steps of a part at least.  A part costs its start, its results and their joining: shorter ones than 256 keys lose.
 __device__ __forceinline__ int least_steps(const DenseArgs& a) { return 256 / a.keys; }
+// Parts of a tile: ceil(steps / chunk), but 64 at most, which is as many as are joined in a few us.
+constexpr int MOST_PARTS = 64;
+__device__ __forceinline__ int parts_of(const DenseArgs& a, int chunk, int keys) {
+  return chunk == 0 ? 1 : min(MOST_PARTS, max(1, (steps_of(a, keys) + chunk - 1) / chunk));
+}
+
+// Steps of a part where tiles are cut, 0 where not: `tiles` and `steps` of all sequences, for each head of keys.  Uncut, the call lasts as long as the
+// longest tile, or as its rounds of workgroups; cut, as a workgroup's share of the steps and the joining.  16 rows, which wait for memory: halves of a
+// share, so that the workgroups end together (16 sequences of 1 to 8192 keys x 8 heads 123 us uncut, 51 in shares, 49.5 in halves; 16 x 3000 x 40 217, 220,
+// 194; 400 tiles of 500 keys 30, 41, 40).  128 rows: a lone workgroup on a compute unit takes a third of the time a step that it takes
+// beside two others, and results of parts are 64 KB (12000 rows, one head, 244 us uncut, 85 in shares, 106 in halves; 4096 x 12 108, 107, 117; 1024 x 40, not
+// causal, 47, 58, 64; 6 x 700 x 12 40, 52, 53).
+__device__ __forceinline__ int chunk_of(const DenseArgs& a, int64_t tiles, float steps, float longest) {
+  const int64_t all = tiles * a.kv_heads;
+  if (!a.may_split || all >= 2 * a.workgroups || tiles == 0) return 0;
+  const bool rows = a.tile == 16;
+  const float share = steps * (float)a.kv_heads / (float)a.workgroups, rounds = (float)((all + a.workgroups - 1) / a.workgroups);
+  if (rows ? fmaxf(longest, rounds * steps / (float)tiles) <= 1.15f * share + 4.f : longest <= 3.f * share + 8.f) return 0;
+  return max((int)ceilf(rows ? 0.5f * share : share), least_steps(a));
+}
 
 // Sum over this lane and those in front of it.
 __device__ __forceinline__ int lanes_scan(int v) {
@@ -216,21 +239,21 @@ __device__ __forceinline__ Work work_of_lane(const DenseArgs& a) {
   w.parts = 1;
   w.items_before = w.tiles_before;
   const int all = __builtin_amdgcn_readlane(w.tiles_before, 63);
-  if (!a.may_split || all < 0 || (int64_t)all * a.kv_heads >= a.workgroups) return w;
+  if (!a.may_split || all < 0) return w;
   float steps = 0.f;   // of all tiles of the sequence: from the first one's to the last one's
   if (w.tiles > 0) steps = 0.5f * (float)w.tiles * ((float)steps_of(a, keys_of_tile(a, w.n, 0)) + (float)steps_of(a, w.n.nk));
-  const float total = wave_sum_f32(steps) * (float)a.kv_heads;
-  w.chunk = max((int)ceilf(total / (float)a.workgroups), least_steps(a));
-  w.parts = max(1, (steps_of(a, w.n.nk) + w.chunk - 1) / w.chunk);
+  float longest = w.tiles > 0 ? (float)steps_of(a, w.n.nk) : 0.f;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) longest = fmaxf(longest, __shfl_xor(longest, d));
+  w.chunk = chunk_of(a, all, wave_sum_f32(steps), longest);
+  if (w.chunk == 0) return w;
+  w.parts = parts_of(a, w.chunk, w.n.nk);
   w.items_before = lanes_scan(w.tiles * w.parts);
   return w;
 }
 __device__ __forceinline__ Lengths lengths_from(const Lengths& n, int lane) {
   return {__builtin_amdgcn_readlane(n.q0, lane), __builtin_amdgcn_readlane(n.nq, lane), __builtin_amdgcn_readlane(n.kv0, lane),
           __builtin_amdgcn_readlane(n.nk, lane)};
-}
-__device__ __forceinline__ int parts_of(const DenseArgs& a, int chunk, int keys) {
-  return chunk == 0 ? 1 : max(1, (steps_of(a, keys) + chunk - 1) / chunk);
 }
 // Item `index` of the call, the same for all lanes; false: there is none.  Slots past the last one: starts that do not ascend.
 __device__ __forceinline__ bool find_item(const DenseArgs& a, int index, DenseItem* item) {
@@ -325,22 +348,32 @@ __global__ __launch_bounds__(1024) void dense_plan_kernel(DenseArgs a) {
     return item_of(a, n, tiles_of(a, n), j - bins[s]);
   };
   const int n_tiles = (int)min(tiles, (int64_t)a.max_tiles);   // more only where starts do not ascend
-  if (!a.may_split || tiles * a.kv_heads >= a.workgroups) {
+  // fewer tiles than may be cut, 1024 at most: their steps
+  DenseItem mine = {};
+  int steps = 0, chunk = 0;
+  if (a.may_split && tiles * a.kv_heads < 2 * a.workgroups && n_tiles <= 1024) {
+    if (tid < n_tiles) {
+      mine = tile_at_index(tid);
+      steps = steps_of(a, mine.end);
+    }
+    int64_t all;
+    scan(steps, room, &all);
+    float longest = (float)steps;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) longest = fmaxf(longest, __shfl_xor(longest, d));
+    __syncthreads();
+    if ((tid & 63) == 0) first_item[tid >> 6] = (int)longest;
+    __syncthreads();
+    for (int i = 0; i < 16; ++i) longest = fmaxf(longest, (float)first_item[i]);
+    __syncthreads();
+    chunk = chunk_of(a, n_tiles, (float)all, longest);
+  }
+  if (chunk == 0) {
     for (int j = tid; j < n_tiles; j += 1024) a.items[j] = tile_at_index(j);
     if (tid == 0) a.counts[0] = n_tiles, a.counts[1] = 0;
     return;
   }
-  // fewer tiles than workgroups wanted (1024 at most): cut into parts of equal length
-  DenseItem mine = {};
-  int steps = 0;
-  if (tid < n_tiles) {
-    mine = tile_at_index(tid);
-    steps = steps_of(a, mine.end);
-  }
-  int64_t all;
-  scan(steps, room, &all);
-  const int chunk = (int)max((all * a.kv_heads + a.workgroups - 1) / a.workgroups, (int64_t)least_steps(a));
-  const int parts = tid < n_tiles ? max((steps + chunk - 1) / chunk, 1) : 0;
+  const int parts = tid < n_tiles ? parts_of(a, chunk, mine.end) : 0;
   int64_t n_items, n_slots, n_merges;
   const int item0 = (int)scan(parts, room, &n_items);
   const int slot0 = (int)scan(parts > 1 ? parts : 0, room, &n_slots);
@@ -396,8 +429,8 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(Dens
   typedef typename Type<T>::eight eight;
   constexpr int KEYS = 64, KS = D / 16, DT = D / 32, MH = KEYS / 32, PH = KEYS / 16, CH = D / 8;
   constexpr int CHUNKS = KEYS * CH, COPIES = CHUNKS / 256, ROWS_PER_COPY = 256 / CH;
-  __shared__ __attribute__((aligned(256))) u32x4 Ks[CHUNKS];
-  __shared__ __attribute__((aligned(256))) u32x4 Vs[CHUNKS];
+  __shared__ __attribute__((aligned(256))) u32x4 Ks[2 * CHUNKS];
+  u32x4* Vs = Ks + CHUNKS;
   const int index = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - index * a.kv_heads;
   DenseItem it;
   if (!find_item(a, index, &it)) return;
@@ -550,44 +583,53 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(Dens
 
   // lane holds channels 32 dt + 8 g + 4 hl + 0..3 of its row
   const float l_all = l_run + __shfl_xor(l_run, 32);
-  if (it.slot >= 0) {
-    if (!r.there) return;
-    const int64_t at = ((int64_t)it.slot * a.kv_heads + kv_head) * 128 + 32 * wave + ql;
-    float* o = a.part + at * D + 4 * hl;
+  if (it.slot >= 0) {   // as they lie in the registers: whole kilobytes
+    const int64_t at = ((int64_t)it.slot * a.kv_heads + kv_head) * 128 + 32 * wave;
+    f32x4* o = (f32x4*)(a.part + at * D) + lane;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) *(float4*)(o + 32 * dt + 8 * g) = make_float4(O[dt][4 * g], O[dt][4 * g + 1], O[dt][4 * g + 2], O[dt][4 * g + 3]);
-    if (hl == 0) a.stat[2 * at] = m_run, a.stat[2 * at + 1] = l_all;
+      for (int g = 0; g < 4; ++g) o[(dt * 4 + g) * 64] = (f32x4){O[dt][4 * g], O[dt][4 * g + 1], O[dt][4 * g + 2], O[dt][4 * g + 3]};
+    if (hl == 0) *(f32x2*)(a.stat + 2 * (at + ql)) = (f32x2){reference_of(m_run, l_all), l_all};
     return;
   }
-  if (!r.there) return;
+  // Through LDS, so that a store takes whole rows: stored from here, 16 bytes of 32 rows at a time, texts took 200 us instead of @.
   const float inv = l_all > 0.f ? 1.0f / l_all : l_all == 0.f ? 0.f : l_all;   // NaN stays
-  uint16_t* out = a.out + r.token * a.out_row + (int64_t)r.head * a.out_head + 4 * hl;
-  struct __attribute__((packed, aligned(2))) Piece8 {
-    uint32_t w[2];
-  };
+  __syncthreads();   // every wavefront has read K and V
+  const uint32_t room = lds_address(Ks) + wave * (64 * D);   // 32 rows
+  auto turned = [](int row) { return D == 128 ? row & 15 : row & 7; };
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      Piece8 w = {{Type<T>::pack(O[dt][4 * g] * inv, O[dt][4 * g + 1] * inv), Type<T>::pack(O[dt][4 * g + 2] * inv, O[dt][4 * g + 3] * inv)}};
-      *(Piece8*)(out + 32 * dt + 8 * g) = w;
+      const u32x2 w = {Type<T>::pack(O[dt][4 * g] * inv, O[dt][4 * g + 1] * inv), Type<T>::pack(O[dt][4 * g + 2] * inv, O[dt][4 * g + 3] * inv)};
+      *(__attribute__((address_space(3))) u32x2*)(uintptr_t)(room + ql * (2 * D) + ((4 * dt + g) ^ turned(ql)) * 16 + hl * 8) = w;
     }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int n = lane / CH; n < 32; n += 64 / CH) {
+    const Row to = row_at(a, it, kv_head, it.row0 + 32 * wave + n);
+    const u32x4 w = piece16(room + n * (2 * D) + ((lane % CH) ^ turned(n)) * 16);
+    if (to.there) {
+      store_once(a.out + to.token * a.out_row + (int64_t)to.head * a.out_head + lane % CH * 8, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+  }
 }
 
 // ---- tiles of 16 rows
 
-// Few rows: the keys are read once and are what takes the time.  Each of the four wavefronts takes 32 keys of every 128 with LDS of its own,
-// two steps deep, so that nothing but its own copies makes it wait; the four join at the end.
+constexpr int ROWS_WAVES = 2;
+
+// Few rows: the keys are read once and are what takes the time.  Each wavefront takes 32 keys of every 32 x WAVES with LDS of its own,
+// two steps deep, so that nothing but its own copies makes it wait; they join at the end.
 template <typename T, int D, bool ALIGNED>
-__global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
+__global__ __launch_bounds__(64 * ROWS_WAVES) void dense_rows_kernel(DenseArgs a) {
   typedef typename Type<T>::eight eight;
-  constexpr int KEYS = 32, KS = D / 32, DT = D / 16, CH = D / 8, BYTES = KEYS * D * 2, STAGES = 2;
+  constexpr int WAVES = ROWS_WAVES, KEYS = 32, KS = D / 32, DT = D / 16, CH = D / 8, BYTES = KEYS * D * 2, STAGES = 2;
   constexpr int COPIES = BYTES / 1024, ROWS_PER_COPY = 64 / CH;   // of a wavefront, for K
   constexpr int ROOM = STAGES * 2 * BYTES;                        // of a wavefront
-  __shared__ __attribute__((aligned(256))) uint8_t tiles[4 * ROOM];
-  __shared__ float stats[4][16][2];
+  __shared__ __attribute__((aligned(256))) uint8_t tiles[WAVES * ROOM];
+  __shared__ float stats[WAVES][16][2];
   static_assert(ROOM >= 16 * D * 4, "");
   const int index = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - index * a.kv_heads;
   DenseItem it;
@@ -643,9 +685,9 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
   int key = first_key, stage = 0;
   if (key < it.end) {
     copy_step(key, 0);
-    copy_step(key + 4 * KEYS, 1);
+    copy_step(key + WAVES * KEYS, 1);
   }
-  for (; key < it.end; key += 4 * KEYS, stage ^= 1) {
+  for (; key < it.end; key += WAVES * KEYS, stage ^= 1) {
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(ALIGNED ? 2 * COPIES : 0) : "memory");
     const uint32_t at = lds + stage * 2 * BYTES;
     const bool masked = key + KEYS > all_see;
@@ -713,12 +755,12 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul16(__builtin_bit_cast(eight, v_fragment(dt)), pb, O[dt]);
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // this stage has been read
-    copy_step(key + 8 * KEYS, stage);
+    copy_step(key + 2 * WAVES * KEYS, stage);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");   // nothing is on its way into LDS
 
   if (a.causal && __ballot(taken) != 0) {   // what was taken out, to the rows that see it: it makes of a sum what it is itself
-    for (int step = first_key; step < it.end; step += 4 * KEYS) {
+    for (int step = first_key; step < it.end; step += WAVES * KEYS) {
       if (step + KEYS <= all_see) continue;
       for (int j = step; j < min(min(step + KEYS, it.end), r.limit); ++j) {
         const T* v = (const T*)v0 + (int64_t)j * a.v_row + 4 * g;
@@ -730,51 +772,52 @@ __global__ __launch_bounds__(256) void dense_rows_kernel(DenseArgs a) {
     }
   }
 
-  // the four wavefronts' results
+  // the wavefronts' results
   l_run += __shfl_xor(l_run, 16);
   l_run += __shfl_xor(l_run, 32);
-  if (lane < 16) stats[wave][i16][0] = m_run, stats[wave][i16][1] = l_run;
+  if (lane < 16) stats[wave][i16][0] = reference_of(m_run, l_run), stats[wave][i16][1] = l_run;
   float* mine = (float*)(tiles + wave * ROOM) + i16 * D + 4 * g;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) *(f32x4*)(mine + 16 * dt) = O[dt];
   __syncthreads();
-  const int row = tid >> 4, c0 = (tid & 15) * (D / 16);   // a thread: D / 16 channels of a row
+  constexpr int PER_ROW = 4 * WAVES, N = D / PER_ROW;   // threads of a row, channels of a thread
+  const int row = tid / PER_ROW, c0 = tid % PER_ROW * N;
   const Row to = row_at(a, it, kv_head, it.row0 + row);
   if (!to.there) return;
-  float m_all = -__builtin_inff(), l_all = 0.f, o[D / 16] = {};
+  float m_all = -__builtin_inff(), l_all = 0.f, o[N] = {};
 #pragma unroll
-  for (int w = 0; w < 4; ++w)
+  for (int w = 0; w < WAVES; ++w)
     if (stats[w][row][1] != 0.f) m_all = fmaxf(m_all, stats[w][row][0]);   // NaN is not 0
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < WAVES; ++w) {
     const float l = stats[w][row][1];
     if (l == 0.f) continue;
     const float by = exp2_of(stats[w][row][0] - m_all);
     l_all = fmaf(l, by, l_all);
     const float* from = (const float*)(tiles + w * ROOM) + row * D + c0;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) o[i] = fmaf(from[i], by, o[i]);
+    for (int i = 0; i < N; ++i) o[i] = fmaf(from[i], by, o[i]);
   }
   if (it.slot >= 0) {
     const int64_t n = ((int64_t)it.slot * a.kv_heads + kv_head) * 16 + row;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) a.part[n * D + c0 + i] = o[i];
-    if ((tid & 15) == 0) a.stat[2 * n] = l_all == 0.f ? 0.f : m_all, a.stat[2 * n + 1] = l_all;
+    for (int i = 0; i < N; i += 4) *(f32x4*)(a.part + n * D + c0 + i) = (f32x4){o[i], o[i + 1], o[i + 2], o[i + 3]};
+    if (tid % PER_ROW == 0) a.stat[2 * n] = l_all == 0.f ? 0.f : m_all, a.stat[2 * n + 1] = l_all;
     return;
   }
   const float inv = l_all > 0.f ? 1.0f / l_all : l_all == 0.f ? 0.f : l_all;
   T* out = (T*)a.out + to.token * a.out_row + (int64_t)to.head * a.out_head + c0;
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) out[i] = (T)(o[i] * inv);
+  for (int i = 0; i < N; ++i) out[i] = (T)(o[i] * inv);
 }
 
 // ---- joining
 
-// A wavefront a row of a tile that was cut: a lane looks at a part's reference and sum, 64 of them at a time, then groups of lanes with four
+// Tiles of 16 rows: a wavefront a row, a lane looks at a part's reference and sum, 64 of them at a time, then groups of lanes with four
 // channels each take a part each.
-template <typename T, int D, int TILE>
-__global__ __launch_bounds__(256) void dense_merge_kernel(DenseArgs a) {
-  constexpr int LANES = D / 4, GROUPS = 64 / LANES, BLOCKS = TILE / 4;
+template <typename T, int D>
+__global__ __launch_bounds__(256) void dense_merge_rows_kernel(DenseArgs a) {
+  constexpr int TILE = 16, LANES = D / 4, GROUPS = 64 / LANES, BLOCKS = TILE / 4;
   const int block = blockIdx.x % BLOCKS, of = blockIdx.x / BLOCKS, index = of / a.kv_heads, kv_head = of - index * a.kv_heads;
   DenseMerge it;
   if (!find_merge(a, index, &it)) return;
@@ -800,11 +843,15 @@ __global__ __launch_bounds__(256) void dense_merge_kernel(DenseArgs a) {
     l = l * alpha + wave_sum_f32(sum * weight);
     o *= alpha;
     const int n = min(64, it.parts - p0);
-#pragma unroll 4
-    for (int p = group; p < n; p += GROUPS) {
-      const float w = __shfl(weight, p);
-      const f32x4 part = *(const f32x4*)(a.part + (first + step * (p0 + p)) * D + c);
-      if (w != 0.f) o += part * w;
+    for (int q = group; q < n; q += 4 * GROUPS) {   // four at a time; past the last one it again, and not taken
+      f32x4 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = *(const f32x4*)(a.part + (first + step * (p0 + min(q + i * GROUPS, n - 1))) * D + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float w = __shfl(weight, min(q + i * GROUPS, 63));   // weights past the last part are 0
+        if (w != 0.f && q + i * GROUPS < n) o += x[i] * w;
+      }
     }
   }
 #pragma unroll
@@ -819,18 +866,65 @@ __global__ __launch_bounds__(256) void dense_merge_kernel(DenseArgs a) {
   for (int e = 0; e < 4; ++e) out[e] = (T)(o[e] * inv);
 }
 
+// Tiles of 128 rows: a workgroup for 32 of them and 32 channels; a lane has a row and four of the channels.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void dense_merge_tiles_kernel(DenseArgs a) {
+  constexpr int TILE = 128, BLOCKS = 4 * (D / 32);
+  const int block = blockIdx.x % BLOCKS, of = blockIdx.x / BLOCKS, index = of / a.kv_heads, kv_head = of - index * a.kv_heads;
+  DenseMerge it;
+  if (!find_merge(a, index, &it)) return;
+  const int lane = threadIdx.x & 63, wave = block & 3, unit = block / 4 * 4 + (threadIdx.x >> 6), row = 32 * wave + (lane & 31);
+  const int64_t first = ((int64_t)it.slot * a.kv_heads + kv_head) * TILE + 32 * wave, step = (int64_t)a.kv_heads * TILE;
+  const f32x2* stat = (const f32x2*)a.stat + first + (lane & 31);
+  const f32x4* part = (const f32x4*)(a.part + first * D) + unit * 64 + lane;
+  float top = -__builtin_inff(), l = 0.f;
+  // four parts at a time; past the last one it again, and not taken
+  for (int p = 0; p < it.parts; p += 4) {
+    f32x2 s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = stat[step * min(p + i, it.parts - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[i][1] != 0.f ? s[i][0] : -__builtin_inff());   // NaN is not 0
+  }
+  f32x4 o = 0.f;
+  for (int p = 0; p < it.parts; p += 4) {
+    f32x2 s[4];
+    f32x4 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[i] = stat[step * min(p + i, it.parts - 1)];
+      x[i] = part[step * min(p + i, it.parts - 1) * (D / 4)];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float weight = s[i][1] != 0.f && p + i < it.parts ? exp2_of(s[i][0] - top) : 0.f;
+      if (weight != 0.f) {
+        l = fmaf(s[i][1], weight, l);
+        o += x[i] * weight;
+      }
+    }
+  }
+  const uint32_t t = token_of(a, (uint32_t)(it.row0 + row));
+  if ((int)t >= it.nq) return;
+  const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+  const int head = kv_head * a.group + it.row0 + row - (int)t * a.group;
+  T* out = (T*)a.out + ((int64_t)it.q0 + t) * a.out_row + (int64_t)head * a.out_head + 8 * unit + 4 * (lane >> 5);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[e] = (T)(o[e] * inv);
+}
+
 int status() { return hipGetLastError() == hipSuccess ? JENGA_OK : JENGA_EHIP; }
 
 template <typename T, int D, bool ALIGNED>
 int run(const DenseArgs& a, const DenseShape& s, hipStream_t st) {
-  const unsigned grid = (unsigned)(s.items * a.kv_heads), merges = (unsigned)(s.split_tiles * a.kv_heads * (s.rows / 4));
+  const unsigned grid = (unsigned)(s.items * a.kv_heads), merges = (unsigned)(s.split_tiles * a.kv_heads);
   if (a.items) dense_plan_kernel<<<1, 1024, 0, st>>>(a);
   if (s.rows == 16) {
-    dense_rows_kernel<T, D, ALIGNED><<<grid, 256, 0, st>>>(a);
-    if (s.may_split) dense_merge_kernel<T, D, 16><<<merges, 256, 0, st>>>(a);
+    dense_rows_kernel<T, D, ALIGNED><<<grid, 64 * ROWS_WAVES, 0, st>>>(a);
+    if (s.may_split) dense_merge_rows_kernel<T, D><<<4 * merges, 256, 0, st>>>(a);
   } else {
     dense_tiles_kernel<T, D, ALIGNED><<<grid, 256, 0, st>>>(a);
-    if (s.may_split) dense_merge_kernel<T, D, 128><<<merges, 256, 0, st>>>(a);
+    if (s.may_split) dense_merge_tiles_kernel<T, D><<<D / 8 * merges, 256, 0, st>>>(a);
   }
   return status();
 }
@@ -875,7 +969,7 @@ int jenga_dense_attn(const jenga_dense_config* cfg, const void* q, const void* k
   a.causal = (c.flags & JENGA_DENSE_CAUSAL) != 0;
   a.scale_log2e = c.scale * 1.4426950408889634f;
   a.tile = s.rows;
-  a.keys = s.rows == 16 ? 128 : 64;
+  a.keys = s.rows == 16 ? 32 * ROWS_WAVES : 64;
   a.max_tiles = (int32_t)s.tiles;
   a.max_slots = (int32_t)s.slots;
   a.workgroups = (int32_t)s.workgroups;

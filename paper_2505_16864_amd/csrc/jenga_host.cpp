@@ -584,16 +584,16 @@ DenseShape dense_shape(const jenga_dense_config& c) {
   DenseShape s;
   const int64_t group = c.heads / c.kv_heads, rows = c.q_rows * group;
   s.rows = rows <= 32 * (int64_t)c.sequences ? 16 : 128;
-  s.workgroups = s.rows == 16 ? 512 : 768;
+  s.workgroups = s.rows == 16 ? 512 : c.head_dim == 128 ? 768 : 1024;   // that the chip holds, or that keep its memory busy
   // each sequence ends with a tile that may not be full
   s.tiles = rows == 0 ? 0 : rows / s.rows + c.sequences;
   // full tiles that there are at least
   const int64_t least = rows / s.rows;
-  s.may_split = least * c.kv_heads < s.workgroups;
+  s.may_split = least * c.kv_heads < 2 * s.workgroups;
   s.listed = c.sequences > 64;
-  // A tile of n steps makes ceil(n / chunk) parts, and the steps of all tiles are workgroups / kv_heads chunks at most.  Without a list the tiles of a
+  // A tile of n steps makes ceil(n / chunk) parts, and a chunk is half of a workgroup's share of the steps at least.  Without a list the tiles of a
   // sequence have as many places as the longest has parts, and their steps are taken as half of that at least; sums are float32 there.
-  const int64_t split = (s.workgroups + c.kv_heads - 1) / c.kv_heads, chunks = s.listed ? split : 2 * split + 16;
+  const int64_t split = (2 * s.workgroups + c.kv_heads - 1) / c.kv_heads, chunks = s.listed ? split : 2 * split + 16;
   s.split_tiles = s.may_split ? std::min<int64_t>(s.tiles, split) : 0;
   s.slots = s.may_split ? s.split_tiles + chunks : 0;
   s.items = std::max<int64_t>(s.tiles, s.slots);

@@ -135,6 +135,17 @@ def test_what_is_not_seen(q_lens, kv_lens, heads, kv_heads, dtype, d):
     assert bool(torch.isnan(got[q_lens[0] - 1, 0]).all())
 
 
+# A key that makes NaN of a row does so however far its part's other logits lie below those of other parts.
+@pytest.mark.parametrize("q_len", [1, 100])
+def test_nan_among_small_logits(q_len):
+    n = 4000
+    q, k, v = _inputs(q_len, n, 1, 1, 64, "bf16", 21)
+    q[:, 0, 0], k[:, 0, 0] = 4.0, 60.0
+    k[:2000, 0, 0] = -60.0
+    k[700, 0, 5] = float("nan")
+    assert bool(torch.isnan(_run(q, k, v, [q_len], [n], False)).all())
+
+
 # Logits that climb and fall along the keys by hundreds, so that the reference has to move, in either type; constant rows.
 @pytest.mark.parametrize("q_len", [1, 150])
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 128), ("f16", 64)])
