@@ -129,11 +129,20 @@ __global__ __launch_bounds__(512) void matmul_mx_rows_kernel(MatmulArgs g) {
   }
 }
 
-// 64 lanes x 4 bytes from a buffer.
-__device__ __forceinline__ void copy_dwords(const u32x4& buffer, uint32_t lane_offset, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+// 64 lanes x 4 or 16 bytes from a buffer, or nothing: without a branch, which would part the products from the reads and copies between them.
+// Pieces of 16 bytes may lie on any multiple of four.
+__device__ __forceinline__ void copy_dwords(bool wanted, const u32x4& buffer, uint32_t lane_offset, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %4\n\ts_mov_b32 exec_hi, %4\n\tbuffer_load_dword %1, %2, %3 offen lds\n\ts_mov_b64 exec, -1"
                :
-               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(lane_offset), "s"(buffer), "s"(offset)
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(lane_offset), "s"(buffer), "s"(__builtin_amdgcn_readfirstlane(offset)),
+                 "s"(__builtin_amdgcn_readfirstlane(wanted ? -1 : 0))
+               : "memory", "m0");
+}
+__device__ __forceinline__ void copy_pieces(bool wanted, const u32x4& buffer, uint32_t lane_offset, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_mov_b32 exec_lo, %4\n\ts_mov_b32 exec_hi, %4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds\n\ts_mov_b64 exec, -1"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(lane_offset), "s"(buffer), "s"(__builtin_amdgcn_readfirstlane(offset)),
+                 "s"(__builtin_amdgcn_readfirstlane(wanted ? -1 : 0))
                : "memory", "m0");
 }
 
@@ -147,16 +156,18 @@ __device__ __forceinline__ void copy_dwords(const u32x4& buffer, uint32_t lane_o
 // row, so that the rows of a fragment fall on all banks.  The rows of b are the rows of the matrix instruction, taken in an order that puts eight
 // neighbouring results of a row of out into a lane: two fragments j, j + 1 hold columns 16 q + 8 (lane / 32) + 4 (j & 1) + 0..3 of 64.
 // A lane has pieces 2 h and 2 h + 1 of a half row, h = lane / 32: two products, whose scales are those two bytes of the half row's four.
-// Scales are copied a half row at a time, the 64 rows of an instruction next to each other.
-template <typename O, int BM, int BN, int STAGES>
+// Scales are copied 16 bytes a row, which serve four halves, in every other block; the last ones of a row end with it.  (Four bytes a row
+// and instruction, 64 cache lines each: 33272 x 15360 x 5120 1646 us, 1231 without any.)  SHORT: rows of less than 16 bytes.
+template <typename O, int BM, int BN, int STAGES, bool SHORT>
 __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
   constexpr int WM = 2, WN = 2, MT = BM / WM / 32, NT = BN / WN / 32, COPIES = (BM + BN) / 32, STAGE = (BM + BN) * 128;
-  constexpr int SCALE_COPIES = 4, ALL = COPIES + SCALE_COPIES, SCALE_STAGE = (BM + BN) * 8;   // of a wavefront and block
+  constexpr int SCALE_COPIES = SHORT ? 6 : 2, ALL = COPIES + SCALE_COPIES;   // of a wavefront and block
+  constexpr int SCALE_ROOM = (BM + BN) * 16, SCALE_ROOMS = STAGES / 2 + 1;
   static_assert(STAGES >= 2 && STAGES <= 4 && BM % 64 == 0 && BN % 64 == 0 && BN / WN <= 128 && 128 % (BN / WN) == 0 && NT % 2 == 0, "");
   // the results of 32 rows of each wavefront go where the tiles but the first are
   constexpr int PITCH = BN / WN * sizeof(O), REST = (STAGES - 1) * STAGE, SECOND = REST > 4 * 32 * PITCH ? REST : 4 * 32 * PITCH;
-  constexpr int SCALES = STAGE + SECOND;   // [STAGES][2][BM + BN] four bytes each
-  __shared__ __attribute__((aligned(128))) uint8_t tiles[SCALES + STAGES * SCALE_STAGE];
+  constexpr int SCALES = STAGE + SECOND;   // [SCALE_ROOMS][BM + BN][16], SHORT: [.][4][BM + BN][4]
+  __shared__ __attribute__((aligned(128))) uint8_t tiles[SCALES + SCALE_ROOMS * SCALE_ROOM];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
   const uint32_t pitch = (uint32_t)g.halves * 64, scale_pitch = (uint32_t)g.halves * 4,
                  lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)tiles;
@@ -198,13 +209,17 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
       copy_1kb(of_a ? a_rows : b_rows, lane_from,
                s < g.steps ? (of_a ? c : c - BM / 32) * 32 * pitch + s * 128 : 0x80000000u,   // past the end: outside
                lds0 + (uint32_t)s % STAGES * STAGE + (c * 4 + wave) * 1024);
-    } else {   // four scales of 64 rows: a half, an operand; of an operand with less than four times 64 rows, some of them twice
-      const int half = (c - COPIES) >> 1;
+    } else {   // of 64 rows of an operand; where that has less than four times 64, of some of them twice
       const bool of_a = (c & 1) == 0;
-      const int r = wave * 64 % (of_a ? BM : BN);
-      copy_dwords(of_a ? a_scales : b_scales, (uint32_t)(lane + r) * scale_pitch,
-                  2 * s + half < g.halves ? (uint32_t)(s * 8 + half * 4) : 0x80000000u,
-                  lds0 + SCALES + (uint32_t)s % STAGES * SCALE_STAGE + (half * (BM + BN) + (of_a ? 0 : BM) + r) * 4);
+      const int r = wave * 64 % (of_a ? BM : BN), half = (c - COPIES) >> 1;
+      const uint32_t to = lds0 + SCALES + (uint32_t)(s >> 1) % SCALE_ROOMS * SCALE_ROOM;
+      const u32x4& scales = of_a ? a_scales : b_scales;
+      const int row = r + (of_a ? 0 : BM);
+      if constexpr (SHORT)
+        copy_dwords((s & 1) == 0, scales, (uint32_t)(lane + r) * scale_pitch, half < g.halves - 2 * s ? (uint32_t)(s * 8 + half * 4) : 0x80000000u,
+                    to + (half * (BM + BN) + row) * 4);
+      else
+        copy_pieces((s & 1) == 0, scales, (uint32_t)(lane + r) * scale_pitch, (uint32_t)min(2 * s, g.halves - 4) * 4, to + row * 16);
     }
   };
 
@@ -219,8 +234,12 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
     const uint8_t* p = tiles + (uint32_t)s % STAGES * STAGE + H * 512 + (OF_A ? at_a + I * 4096 : at_b + (J >> 1) * 8192 + (J & 1) * 256);
     const uint4 v[2] = {*(const uint4*)(p + (piece ^ turn)), *(const uint4*)(p + ((piece + 16) ^ turn))};
     __builtin_memcpy(OF_A ? &fa[H][I] : &fb[H][J], v, 32);
-    const uint8_t* scales = tiles + SCALES + (uint32_t)s % STAGES * SCALE_STAGE + (H * (BM + BN) + (OF_A ? ra + 32 * I : BM + rb + 64 * (J >> 1) + 4 * (J & 1))) * 4;
-    (OF_A ? scale_a[H][I] : scale_b[H][J]) = (int)(*(const uint32_t*)scales >> (lane >> 5) * 16);   // this lane's two of the half row's four
+    // this lane's two of the half row's four; none behind the last half, where the bytes are another's
+    const int row = OF_A ? ra + 32 * I : BM + rb + 64 * (J >> 1) + 4 * (J & 1), n = 2 * s + H, u = s >> 1;
+    const uint8_t* scales = tiles + SCALES + (uint32_t)u % SCALE_ROOMS * SCALE_ROOM;
+    scales += SHORT ? ((n & 3) * (BM + BN) + row) * 4 : row * 16 + (n - min(4 * u, g.halves - 4)) % 4 * 4;
+    const uint32_t four = *(const uint32_t*)scales & (n < g.halves ? ~0u : 0u);
+    (OF_A ? scale_a[H][I] : scale_b[H][J]) = (int)(four >> (lane >> 5) * 16);
   };
   using std::integral_constant;
   constexpr integral_constant<int, 0> n0;
@@ -243,7 +262,7 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
     });
     // this wavefront's copies of the next block are done (those of later blocks may be on their way), and its reads of this one;
     // then everybody's are
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((STAGES - 2) * ALL) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((STAGES - 2) * COPIES) : "memory");
     __builtin_amdgcn_sched_barrier(0);
     each<PRODUCTS>([&](auto index) {
       constexpr int N = decltype(index)::value;
@@ -323,12 +342,12 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
 
   begin_copies(t);
   each<ALL>([&](auto c) { copy_one(0, decltype(c)::value); });
-  constexpr int BEHIND = (STAGES - 1) * ALL + STORES < 63 ? (STAGES - 1) * ALL + STORES : 63;   // or fewer: what was issued behind block 0
+  constexpr int BEHIND = (STAGES - 1) * COPIES + STORES < 63 ? (STAGES - 1) * COPIES + STORES : 63;   // what was issued behind block 0 at least: a copy of scales may be none
   bool stores_under_way = false;
   for (;;) {
     each<(STAGES - 1) * ALL>([&](auto c) { copy_one(1 + decltype(c)::value / ALL, decltype(c)::value % ALL); });
     if (stores_under_way) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(BEHIND) : "memory");   // they are behind block 0
-    else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((STAGES - 1) * ALL) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((STAGES - 1) * COPIES) : "memory");
     each<READS>([&](auto r) { read_one(0, n0, r); });
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -353,12 +372,12 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
 
 // per_cu: workgroups that a compute unit holds, by LDS.  A workgroup makes several tiles, so that the first block of the next one is on its
 // way while the results of the last one are stored.
-template <typename O, int BM, int BN, int STAGES>
+template <typename O, int BM, int BN, int STAGES, bool SHORT = false>
 int run_tiles(MatmulArgs g, int per_cu, hipStream_t st) {
   g.tiles_m = (int)((g.m + BM - 1) / BM);
   g.tiles_n = (g.n + BN - 1) / BN;
   const int tiles = (g.tiles_m * g.tiles_n + 7) / 8 * 8;
-  matmul_mx_kernel<O, BM, BN, STAGES><<<std::min(tiles, 256 * per_cu), 256, 0, st>>>(g);
+  matmul_mx_kernel<O, BM, BN, STAGES, SHORT><<<std::min(tiles, 256 * per_cu), 256, 0, st>>>(g);
   return status();
 }
 
@@ -373,6 +392,7 @@ int run_matmul(const MatmulArgs& g, hipStream_t st) {
   const jenga::MatmulTiles t = jenga::matmul_mx_tiles(g.m, g.n);
   if (t.rows == 16) return run_rows<O, 1>(g, st);
   if (t.rows == 32) return run_rows<O, 2>(g, st);
+  if (g.halves < 4) return run_tiles<O, 64, 128, 4, true>(g, 1, st);
   if (t.bm == 256) return run_tiles<O, 256, 256, 2>(g, t.per_cu, st);
   if (t.bm == 64) return run_tiles<O, 64, 128, 4>(g, t.per_cu, st);
   if (t.stages == 4) return run_tiles<O, 128, 128, 4>(g, t.per_cu, st);
