@@ -157,7 +157,9 @@ __device__ __forceinline__ void copy_pieces(bool wanted, const u32x4& buffer, ui
 // neighbouring results of a row of out into a lane: two fragments j, j + 1 hold columns 16 q + 8 (lane / 32) + 4 (j & 1) + 0..3 of 64.
 // A lane has pieces 2 h and 2 h + 1 of a half row, h = lane / 32: two products, whose scales are those two bytes of the half row's four.
 // Scales are copied 16 bytes a row, which serve four halves, in every other block; the last ones of a row end with it.  (Four bytes a row
-// and instruction, 64 cache lines each: 33272 x 15360 x 5120 1646 us, 1231 without any.)  SHORT: rows of less than 16 bytes.
+// and instruction, 64 cache lines each: 33272 x 15360 x 5120 1646 us; 32 bytes 1483 where 16 take 1474.)  SHORT: rows of less than 16 bytes.  In LDS
+// the rows of b lie as fragments want them, and a lane reads both halves' scales of a row at once: four bytes from every second row's, as they lie in
+// memory, had up to four lanes on a bank.
 template <typename O, int BM, int BN, int STAGES, bool SHORT>
 __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
   constexpr int WM = 2, WN = 2, MT = BM / WM / 32, NT = BN / WN / 32, COPIES = (BM + BN) / 32, STAGE = (BM + BN) * 128;
@@ -167,7 +169,7 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
   // the results of 32 rows of each wavefront go where the tiles but the first are
   constexpr int PITCH = BN / WN * sizeof(O), REST = (STAGES - 1) * STAGE, SECOND = REST > 4 * 32 * PITCH ? REST : 4 * 32 * PITCH;
   constexpr int SCALES = STAGE + SECOND;   // [SCALE_ROOMS][BM + BN][16], SHORT: [.][4][BM + BN][4]
-  __shared__ __attribute__((aligned(128))) uint8_t tiles[SCALES + SCALE_ROOMS * SCALE_ROOM];
+  __shared__ __attribute__((aligned(128))) uint8_t tiles[SCALES + SCALE_ROOMS * SCALE_ROOM + 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave % WM, wn = wave / WM;
   const uint32_t pitch = (uint32_t)g.halves * 64, scale_pitch = (uint32_t)g.halves * 4,
                  lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)tiles;
@@ -201,6 +203,7 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
     a_scales = buffer_of(g.a_scale + row0 * scale_pitch, (uint32_t)rows * scale_pitch);
     b_scales = buffer_of(g.b_scale + (int64_t)col0 * scale_pitch, (uint32_t)cols * scale_pitch);
   };
+  const uint32_t scales_a = lane * scale_pitch, scales_b = (4 * (lane >> 5) + 2 * (lane & 28) + (lane & 3)) * scale_pitch;
   auto copy_one = [&](int s, int c) {
     if (c < COPIES) {
       const bool of_a = c * 32 < BM;
@@ -216,16 +219,21 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
       const u32x4& scales = of_a ? a_scales : b_scales;
       const int row = r + (of_a ? 0 : BM);
       if constexpr (SHORT)
-        copy_dwords((s & 1) == 0, scales, (uint32_t)(lane + r) * scale_pitch, half < g.halves - 2 * s ? (uint32_t)(s * 8 + half * 4) : 0x80000000u,
+        copy_dwords((s & 1) == 0, scales, of_a ? scales_a : scales_b,
+                    half < g.halves - 2 * s ? (uint32_t)r * scale_pitch + (uint32_t)(s * 8 + half * 4) : 0x80000000u,
                     to + (half * (BM + BN) + row) * 4);
       else
-        copy_pieces((s & 1) == 0, scales, (uint32_t)(lane + r) * scale_pitch, (uint32_t)min(2 * s, g.halves - 4) * 4, to + row * 16);
+        copy_pieces((s & 1) == 0, scales, of_a ? scales_a : scales_b, (uint32_t)r * scale_pitch + (uint32_t)min(2 * s, g.halves - 4) * 4, to + row * 16);
     }
   };
 
   f32x16 acc[MT][NT];
   i32x4 fa[2][MT][2], fb[2][NT][2];
-  int scale_a[2][MT], scale_b[2][NT];
+  struct __attribute__((packed, aligned(4))) Two {
+    uint32_t h[2];
+  };
+  Two both[MT + NT];       // as they come: four bytes a half
+  int scale[2][MT + NT];   // this lane's two of them
   // Fragment r of half h of block s: those of b and a in the order in which the products want them.
   auto read_one = [&](int s, auto half, auto index) {
     constexpr int H = decltype(half)::value, R = decltype(index)::value;
@@ -234,27 +242,36 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
     const uint8_t* p = tiles + (uint32_t)s % STAGES * STAGE + H * 512 + (OF_A ? at_a + I * 4096 : at_b + (J >> 1) * 8192 + (J & 1) * 256);
     const uint4 v[2] = {*(const uint4*)(p + (piece ^ turn)), *(const uint4*)(p + ((piece + 16) ^ turn))};
     __builtin_memcpy(OF_A ? &fa[H][I] : &fb[H][J], v, 32);
-    // this lane's two of the half row's four; none behind the last half, where the bytes are another's
-    const int row = OF_A ? ra + 32 * I : BM + rb + 64 * (J >> 1) + 4 * (J & 1), n = 2 * s + H, u = s >> 1;
-    const uint8_t* scales = tiles + SCALES + (uint32_t)u % SCALE_ROOMS * SCALE_ROOM;
-    scales += SHORT ? ((n & 3) * (BM + BN) + row) * 4 : row * 16 + (n - min(4 * u, g.halves - 4)) % 4 * 4;
-    const uint32_t four = *(const uint32_t*)scales & (n < g.halves ? ~0u : 0u);
-    (OF_A ? scale_a[H][I] : scale_b[H][J]) = (int)(four >> (lane >> 5) * 16);
+    if constexpr (H == 0) {   // the scales of both halves; what stands for a half behind the last one is another's
+      const int u = s >> 1, at = (u % SCALE_ROOMS) * SCALE_ROOM + (SHORT ? (2 * s & 3) * (BM + BN) * 4 : ((2 * s - min(4 * u, g.halves - 4)) & 3) * 4);
+      const uint8_t* scales = tiles + SCALES + (OF_A ? (ra + 32 * I) : BM + wn * (BN / WN) + 32 * J + i32) * (SHORT ? 4 : 16) + at;
+      if constexpr (SHORT) both[R] = {*(const uint32_t*)scales, *(const uint32_t*)(scales + (BM + BN) * 4)};
+      else both[R] = *(const Two*)scales;
+    }
   };
   using std::integral_constant;
   constexpr integral_constant<int, 0> n0;
   constexpr integral_constant<int, 1> n1;
   constexpr int PRODUCTS = MT * NT, READS = MT + NT;
+  constexpr auto of_a = [](int i) { return i + 1; };
+  constexpr auto of_b = [](int j) { return j == 0 ? 0 : j + MT; };
+  const int by = (lane >> 5) * 16;
   // Multiplies block s.  Between the products are the reads of the next half and the copies of the block STAGES on.  (Left alone,
   // the compiler reads after the products and waits; all reads and copies before them leave the matrix core without work meanwhile:
   // 8192 x 8192 x 8192 585 -> 445 us.)  What is read and copied behind the last block is not used and not fetched: other code there
   // would cost more, in moves between registers.
   auto block = [&](int s) {
+    const uint32_t there = 2 * s + 1 < g.halves ? ~0u : 0u;
+#pragma unroll
+    for (int r = 0; r < READS; ++r) {
+      scale[0][r] = (int)(both[r].h[0] >> by);
+      scale[1][r] = (int)((both[r].h[1] & there) >> by);
+    }
     each<PRODUCTS>([&](auto index) {
       constexpr int N = decltype(index)::value;
       constexpr int I = N % MT, J = N / MT;
-      acc[I][J] = multiply<0>(fb[0][J][0], scale_b[0][J], fa[0][I][0], scale_a[0][I], acc[I][J]);
-      acc[I][J] = multiply<1>(fb[0][J][1], scale_b[0][J], fa[0][I][1], scale_a[0][I], acc[I][J]);
+      acc[I][J] = multiply<0>(fb[0][J][0], scale[0][of_b(J)], fa[0][I][0], scale[0][of_a(I)], acc[I][J]);
+      acc[I][J] = multiply<1>(fb[0][J][1], scale[0][of_b(J)], fa[0][I][1], scale[0][of_a(I)], acc[I][J]);
       each<READS>([&](auto r) {
         if constexpr (decltype(r)::value * (PRODUCTS - 1) / READS == N) read_one(s, n1, r);
       });
@@ -267,8 +284,8 @@ __global__ __launch_bounds__(256) void matmul_mx_kernel(MatmulArgs g) {
     each<PRODUCTS>([&](auto index) {
       constexpr int N = decltype(index)::value;
       constexpr int I = N % MT, J = N / MT;
-      acc[I][J] = multiply<0>(fb[1][J][0], scale_b[1][J], fa[1][I][0], scale_a[1][I], acc[I][J]);
-      acc[I][J] = multiply<1>(fb[1][J][1], scale_b[1][J], fa[1][I][1], scale_a[1][I], acc[I][J]);
+      acc[I][J] = multiply<0>(fb[1][J][0], scale[1][of_b(J)], fa[1][I][0], scale[1][of_a(I)], acc[I][J]);
+      acc[I][J] = multiply<1>(fb[1][J][1], scale[1][of_b(J)], fa[1][I][1], scale[1][of_a(I)], acc[I][J]);
       each<READS>([&](auto r) {
         if constexpr (decltype(r)::value * (PRODUCTS - 1) / READS == N) read_one(s + 1, n0, r);
       });
