@@ -260,13 +260,15 @@ _EINVAL = -1
 _TYPES = {}            # torch's element types to jenga_type, filled by the first call that needs them
 _DTYPE = {}            # and by name
 _current_device = _current_stream = None
+_U8 = _F32 = _I32 = None
 _MATMUL, _NORM, _TENSOR = struct.Struct("=2q4i"), struct.Struct("=5q4i2f"), struct.Struct("=2Q6q2i")   # as the structures above
 _RMS, _DENSE = struct.Struct("=9q5i2fi"), struct.Struct("=10q5iIfi")
 
 
 def _use_torch():
     import torch
-    global _current_device, _current_stream
+    global _current_device, _current_stream, _U8, _F32, _I32
+    _U8, _F32, _I32 = torch.uint8, torch.float32, torch.int32
     _current_device, _current_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _DTYPE.update(f32=torch.float32, i32=torch.int32, u8=torch.uint8, bf16=torch.bfloat16, e4m3=torch.float8_e4m3fn)
     _TYPES.update({torch.bfloat16: JENGA_BF16, torch.float16: JENGA_F16, torch.float32: JENGA_F32, torch.float8_e4m3fn: JENGA_E4M3,
@@ -451,50 +453,101 @@ def jenga_layer_norm_grad(x, dy, dx, weight, mean, rstd, dweight=None, dbias=Non
                                           0 if workspace is None else workspace.numel() * workspace.element_size(), stream), what)
 
 
+# The calls below are written out where the ones above share helpers: a small one costs what its Python and a launch cost.
+
+def _one_gpu(what, device):
+    """Refuses a call whose tensors are on `device` as far as they have been compared; returns torch's current stream there."""
+    if device < 0:
+        _refuse(what, "tensors are not all on one GPU")
+    if device != _current_device():
+        _refuse(what, "tensors are not on the current device")
+    return _current_stream(device)
+
+
 def jenga_quantize_mx(x, q, scale, stream=None):
     """x [rows, cols] -> 4-bit tensor: q uint8 [rows, padded_columns(cols) / 2], scale uint8 [rows, padded_columns(cols) / 32]."""
     what = "jenga_quantize_mx"
-    stride, kind = _matrix(x, what), _type(x, what)
+    stride, kind = _matrix(x, what), _TYPES.get(x.dtype)
+    if kind is None:
+        kind = _type(x, what)
     rows, cols = x.shape
-    padded = padded_columns(cols)
-    _whole(q, what, (rows, padded // 2), "u8")
-    _whole(scale, what, (rows, padded // 32), "u8")
-    stream = _on_device(what, (x, q, scale), stream)
+    blocks = (cols + 127) >> 7
+    if not (q.dtype is scale.dtype is _U8 and q.shape == (rows, blocks << 6) and scale.shape == (rows, blocks << 2) and q.is_contiguous()
+            and scale.is_contiguous()):
+        _refuse(what, "shapes %s, %s for %d x %d" % (tuple(q.shape), tuple(scale.shape), rows, cols))
+    device = x.get_device()
+    current = _one_gpu(what, device if device == q.get_device() == scale.get_device() else -1)
     if cols > 0x7FFFFFFF:
         _refuse(what, "%d columns" % cols)
     if rows:
-        _check(_lib.jenga_quantize_mx(x.data_ptr(), stride, kind, rows, cols, q.data_ptr(), scale.data_ptr(), stream), what)
+        status = _lib.jenga_quantize_mx(x.data_ptr(), stride, kind, rows, cols, q.data_ptr(), scale.data_ptr(),
+                                        current if stream is None else stream)
+        if status:
+            raise JengaError(status, what)
 
 
 def jenga_matmul_mx(a, a_scale, b, b_scale, out, bias=None, stream=None):
     """out [m, n] = a b^T + bias for 4-bit tensors, a uint8 [m, k / 2] and b uint8 [n, k / 2] with a scale for each 32 values; bias
     float32 [n]."""
     what = "jenga_matmul_mx"
-    if len(a.shape) != 2 or len(b.shape) != 2:
-        _refuse(what, "shapes %s, %s" % (tuple(a.shape), tuple(b.shape)))
-    (m, half), n, kind = a.shape, b.shape[0], _type(out, what)
+    kind, of_a, of_b = _TYPES.get(out.dtype), a.shape, b.shape
+    if kind is None:
+        kind = _type(out, what)
+    if len(of_a) != 2 or len(of_b) != 2:
+        _refuse(what, "shapes %s, %s" % (tuple(of_a), tuple(of_b)))
+    m, half = of_a
+    n = of_b[0]
     stride = _matrix(out, what, m, n)
-    _whole(a, what, (m, half), "u8")
-    _whole(b, what, (n, half), "u8")
-    _whole(a_scale, what, (m, half // 16), "u8")
-    _whole(b_scale, what, (n, half // 16), "u8")
+    if not (of_b[1] == half and a_scale.shape == (m, half >> 4) and b_scale.shape == (n, half >> 4)
+            and a.dtype is b.dtype is a_scale.dtype is b_scale.dtype is _U8
+            and a.is_contiguous() and b.is_contiguous() and a_scale.is_contiguous() and b_scale.is_contiguous()):
+        _refuse(what, "operands of shapes %s, %s with scales %s, %s" % tuple(tuple(t.shape) for t in (a, b, a_scale, b_scale)))
+    device = a.get_device()
+    if not device == b.get_device() == a_scale.get_device() == b_scale.get_device() == out.get_device():
+        device = -1
+    at_bias = None
     if bias is not None:
-        _whole(bias, what, (n,), "f32")
-    stream = _on_device(what, (a, a_scale, b, b_scale, out, bias), stream)
+        if not (bias.dtype is _F32 and bias.shape == (n,) and bias.is_contiguous()):
+            _refuse(what, "bias of shape %s, type %s" % (tuple(bias.shape), bias.dtype))
+        if bias.get_device() != device:
+            device = -1
+        at_bias = bias.data_ptr()
+    current = _one_gpu(what, device)
     if m:
-        _check(_lib.jenga_matmul_mx(_pack(what, _MATMUL, m, stride, n, 2 * half, kind, 0), a.data_ptr(), a_scale.data_ptr(),
-                                    b.data_ptr(), b_scale.data_ptr(), None if bias is None else bias.data_ptr(), out.data_ptr(), stream), what)
+        status = _lib.jenga_matmul_mx(_pack(what, _MATMUL, m, stride, n, 2 * half, kind, 0), a.data_ptr(), a_scale.data_ptr(),
+                                      b.data_ptr(), b_scale.data_ptr(), at_bias, out.data_ptr(), current if stream is None else stream)
+        if status:
+            raise JengaError(status, what)
 
 
-def _heads(t, what, shape=None, dtype=None):
-    """Row and head stride of [rows, cols] or [rows, heads, cols]; along an axis of one any stride will do."""
-    have = t.shape
-    if len(have) not in (2, 3) if shape is None else (have != shape or t.dtype != dtype):
-        _refuse(what, "shape %s, type %s" % (tuple(have), t.dtype))
+def _apart(t, what, shape, dtype, whole):
+    """Row and head stride of a tensor of this shape; `whole`: those of one without gaps.  Along an axis of one any stride will do."""
+    if t.dtype is not dtype or t.shape != shape:
+        _refuse(what, "shape %s, type %s" % (tuple(t.shape), t.dtype))
+    if t.is_contiguous():
+        return whole
     stride = t.stride()
-    if stride[-1] != 1 and have[-1] != 1:
+    if stride[-1] != 1 and shape[-1] != 1:
         _refuse(what, "values of a row are not next to each other")
-    return stride[0] if have[0] > 1 else 0, stride[1] if len(have) == 3 and have[1] > 1 else 0
+    return stride[0] if shape[0] > 1 else 0, stride[1] if len(shape) == 3 and shape[1] > 1 else 0
+
+
+def _rms_sizes(x, what):
+    shape = x.shape
+    if len(shape) == 2:
+        return shape, shape[0], 1, shape[1]
+    if len(shape) != 3:
+        _refuse(what, "shape %s" % (tuple(shape),))
+    return shape, shape[0], shape[1], shape[2]
+
+
+def _rms_weight(weight, what, cols):
+    kind = _TYPES.get(weight.dtype)
+    if kind is None:
+        kind = _type(weight, what)
+    if weight.shape != (cols,) or not weight.is_contiguous():
+        _refuse(what, "weight of shape %s" % (tuple(weight.shape),))
+    return kind
 
 
 def jenga_rms_norm(x, y, weight=None, residual=None, total=None, y_scale=None, rstd=None, weight_offset=0.0, eps=1e-6, stream=None):
@@ -502,44 +555,64 @@ def jenga_rms_norm(x, y, weight=None, residual=None, total=None, y_scale=None, r
     8-bit (e4m3) or 4-bit (uint8) tensor with its scales in y_scale; weight [cols]; rstd float32 [rows] or [rows, heads].  total, or y,
     may be x or residual."""
     what = "jenga_rms_norm"
-    x_type, y_type = _type(x, what), _type(y, what)
-    shape, dtype = x.shape, x.dtype
-    x_row, x_head = _heads(x, what)
-    rows, cols = shape[0], shape[-1]
+    dtype, device = x.dtype, x.get_device()
+    kind = param_type = _TYPES.get(dtype)
+    if kind is None:
+        kind = param_type = _type(x, what)
+    shape, rows, heads, cols = _rms_sizes(x, what)
+    whole = heads * cols, cols
+    x_row, x_head = _apart(x, what, shape, dtype, whole)
     add_row = add_head = sum_row = sum_head = y_row = y_head = 0
+    at_add = at_sum = at_weight = at_scale = at_rstd = None
     if residual is not None:
-        add_row, add_head = _heads(residual, what, shape, dtype)
+        add_row, add_head = _apart(residual, what, shape, dtype, whole)
+        at_add = residual.data_ptr()
+        if residual.get_device() != device:
+            device = -1
     if total is not None:
-        sum_row, sum_head = _heads(total, what, shape, dtype)
+        sum_row, sum_head = _apart(total, what, shape, dtype, whole)
+        at_sum = total.data_ptr()
+        if total.get_device() != device:
+            device = -1
+    y_type = _TYPES.get(y.dtype)
+    if y_type is None:
+        y_type = _type(y, what)
     if y_type == JENGA_E4M3:
         padded = padded_columns(cols)
         if len(shape) != 2 or y_scale is None:
             _refuse(what, "results in 8 and 4 bits are of [rows, cols], with scales")
-        if y.dtype is _DTYPE["u8"]:
+        if y.dtype is _U8:
             y_type = JENGA_E2M1
-            _whole(y, what, (rows, padded // 2), "u8")
-            _whole(y_scale, what, (rows, padded // 32), "u8")
+            _whole(y, what, (rows, padded >> 1), "u8")
+            _whole(y_scale, what, (rows, padded >> 5), "u8")
         else:
             _whole(y, what, (rows, padded), "e4m3")
             _whole(y_scale, what, (rows, scale_columns(cols)), "u8")
+        at_scale = y_scale.data_ptr()
+        if y_scale.get_device() != device:
+            device = -1
     else:
-        y_row, y_head = _heads(y, what, shape, dtype)
+        y_row, y_head = _apart(y, what, shape, dtype, whole)
         if y_scale is not None:
             _refuse(what, "scales of a result that has none")
-    param_type = x_type
     if weight is not None:
-        param_type = _type(weight, what)
-        if weight.shape != shape[-1:] or weight.stride()[0] != 1 and cols != 1:
-            _refuse(what, "weight of shape %s" % (tuple(weight.shape),))
+        param_type = _rms_weight(weight, what, cols)
+        at_weight = weight.data_ptr()
+        if weight.get_device() != device:
+            device = -1
     if rstd is not None:
         _whole(rstd, what, shape[:-1], "f32")
-    stream = _on_device(what, (x, y, weight, residual, total, y_scale, rstd), stream)
-    if rows and (len(shape) == 2 or shape[1]):
-        cfg = _pack(what, _RMS, rows, x_row, x_head, add_row, add_head, sum_row, sum_head, y_row, y_head, shape[1] if len(shape) == 3 else 1,
-                    cols, x_type, y_type, param_type, eps, weight_offset, 0)
-        _check(_lib.jenga_rms_norm(cfg, x.data_ptr(), None if residual is None else residual.data_ptr(),
-                                   None if weight is None else weight.data_ptr(), None if total is None else total.data_ptr(), y.data_ptr(),
-                                   None if y_scale is None else y_scale.data_ptr(), None if rstd is None else rstd.data_ptr(), stream), what)
+        at_rstd = rstd.data_ptr()
+        if rstd.get_device() != device:
+            device = -1
+    current = _one_gpu(what, device if y.get_device() == device else -1)
+    if rows and heads:
+        cfg = _pack(what, _RMS, rows, x_row, x_head, add_row, add_head, sum_row, sum_head, y_row, y_head, heads, cols, kind, y_type, param_type,
+                    eps, weight_offset, 0)
+        status = _lib.jenga_rms_norm(cfg, x.data_ptr(), at_add, at_weight, at_sum, y.data_ptr(), at_scale, at_rstd,
+                                     current if stream is None else stream)
+        if status:
+            raise JengaError(status, what)
 
 
 def jenga_rms_norm_grad_workspace(rows, cols):
@@ -555,31 +628,48 @@ def jenga_rms_norm_grad(total, dy, dx, weight, rstd, dtotal=None, dweight=None, 
     """Gradients of total (what was normed; the same for x and residual) and of weight, float32 [cols], from dy, jenga_rms_norm's rstd and
     dtotal, the gradient that total has from elsewhere.  dx may be dtotal."""
     what = "jenga_rms_norm_grad"
-    kind, shape, dtype = _type(total, what), total.shape, total.dtype
-    x_row, x_head = _heads(total, what)
-    y_row, y_head = _heads(dy, what, shape, dtype)
-    sum_row, sum_head = _heads(dx, what, shape, dtype)
-    rows, cols = shape[0], shape[-1]
+    dtype, device = total.dtype, total.get_device()
+    kind = param_type = _TYPES.get(dtype)
+    if kind is None:
+        kind = param_type = _type(total, what)
+    shape, rows, heads, cols = _rms_sizes(total, what)
+    whole = heads * cols, cols
+    x_row, x_head = _apart(total, what, shape, dtype, whole)
+    y_row, y_head = _apart(dy, what, shape, dtype, whole)
+    sum_row, sum_head = _apart(dx, what, shape, dtype, whole)
     add_row = add_head = 0
+    at_add = at_weight = at_dweight = at_room = None
     if dtotal is not None:
-        add_row, add_head = _heads(dtotal, what, shape, dtype)
-    param_type = kind
+        add_row, add_head = _apart(dtotal, what, shape, dtype, whole)
+        at_add = dtotal.data_ptr()
+        if dtotal.get_device() != device:
+            device = -1
     if weight is not None:
-        param_type = _type(weight, what)
-        if weight.shape != shape[-1:] or weight.stride()[0] != 1 and cols != 1:
-            _refuse(what, "weight of shape %s" % (tuple(weight.shape),))
+        param_type = _rms_weight(weight, what, cols)
+        at_weight = weight.data_ptr()
+        if weight.get_device() != device:
+            device = -1
     if rstd is None:
         _refuse(what, "rstd of the forward pass is wanted")
     _whole(rstd, what, shape[:-1], "f32")
+    room = 0
     if dweight is not None:
-        _whole(dweight, what, shape[-1:], "f32")
-    stream = _on_device(what, (total, dy, dx, weight, rstd, dtotal, dweight, workspace), stream)
-    if rows and (len(shape) == 2 or shape[1]):
-        cfg = _pack(what, _RMS, rows, x_row, x_head, add_row, add_head, sum_row, sum_head, y_row, y_head, shape[1] if len(shape) == 3 else 1,
-                    cols, kind, kind, param_type, 0.0, weight_offset, 0)
-        _check(_lib.jenga_rms_norm_grad(cfg, total.data_ptr(), dy.data_ptr(), _ptr(weight), rstd.data_ptr(), _ptr(dtotal), dx.data_ptr(),
-                                        _ptr(dweight), _ptr(workspace),
-                                        0 if workspace is None else workspace.numel() * workspace.element_size(), stream), what)
+        _whole(dweight, what, (cols,), "f32")
+        at_dweight = dweight.data_ptr()
+        if dweight.get_device() != device:
+            device = -1
+    if workspace is not None:
+        at_room, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        if workspace.get_device() != device:
+            device = -1
+    current = _one_gpu(what, device if device == dy.get_device() == dx.get_device() == rstd.get_device() else -1)
+    if rows and heads:
+        cfg = _pack(what, _RMS, rows, x_row, x_head, add_row, add_head, sum_row, sum_head, y_row, y_head, heads, cols, kind, kind, param_type,
+                    0.0, weight_offset, 0)
+        status = _lib.jenga_rms_norm_grad(cfg, total.data_ptr(), dy.data_ptr(), at_weight, rstd.data_ptr(), at_add, dx.data_ptr(), at_dweight,
+                                          at_room, room, current if stream is None else stream)
+        if status:
+            raise JengaError(status, what)
 
 
 def jenga_dense_attn_workspace(q_rows, kv_rows, sequences, heads, kv_heads, head_dim):
@@ -595,31 +685,44 @@ def jenga_dense_attn(q, k, v, out, q_start, kv_start, kv_len=None, causal=False,
     """q, out [rows, heads, head_dim], k, v [keys, kv_heads, head_dim] (bf16 or fp16, any strides but the last); q_start, kv_start int32
     [sequences + 1], kv_len int32 [sequences], on the device: rows and keys of each sequence.  out may be q.  scale: 1 / sqrt(head_dim)."""
     what = "jenga_dense_attn"
-    kind, shape, keys, dtype = _type(q, what), q.shape, k.shape, q.dtype
+    dtype, shape, keys, device = q.dtype, q.shape, k.shape, q.get_device()
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        kind = _type(q, what)
     if len(shape) != 3 or len(keys) != 3 or keys[2] != shape[2] or not shape[2]:
         _refuse(what, "shapes %s, %s" % (tuple(shape), tuple(keys)))
-    q_row, q_head = _heads(q, what)
-    out_row, out_head = _heads(out, what, shape, dtype)
-    k_row, k_head = _heads(k, what, keys, dtype)
-    v_row, v_head = _heads(v, what, keys, dtype)
+    rows, heads, dim = shape
+    whole, whole_kv = (heads * dim, dim), (keys[1] * dim, dim)
+    q_row, q_head = _apart(q, what, shape, dtype, whole)
+    out_row, out_head = _apart(out, what, shape, dtype, whole)
+    k_row, k_head = _apart(k, what, keys, dtype, whole_kv)
+    v_row, v_head = _apart(v, what, keys, dtype, whole_kv)
     sequences = q_start.numel() - 1
-    if sequences < 0:
-        _refuse(what, "no starts")
-    _whole(q_start, what, (sequences + 1,), "i32")
-    _whole(kv_start, what, (sequences + 1,), "i32")
+    if not (sequences >= 0 and q_start.dtype is kv_start.dtype is _I32 and q_start.shape == kv_start.shape == (sequences + 1,)
+            and q_start.is_contiguous() and kv_start.is_contiguous()):
+        _refuse(what, "starts of shapes %s, %s, types %s, %s" % (tuple(q_start.shape), tuple(kv_start.shape), q_start.dtype, kv_start.dtype))
+    at_len = None
     if kv_len is not None:
         _whole(kv_len, what, (sequences,), "i32")
+        at_len = kv_len.data_ptr()
+        if kv_len.get_device() != device:
+            device = -1
     if workspace is None:
         _refuse(what, "a workspace is wanted")
-    stream = _on_device(what, (q, k, v, out, q_start, kv_start, kv_len, workspace), stream)
-    if shape[0] and shape[1]:
-        cfg = _pack(what, _DENSE, shape[0], keys[0], q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head, sequences, shape[1],
-                    keys[1], shape[2], kind, JENGA_DENSE_CAUSAL if causal else 0, shape[2] ** -0.5 if scale is None else scale, 0)
+    if not device == k.get_device() == v.get_device() == out.get_device() == q_start.get_device() == kv_start.get_device() == \
+            workspace.get_device():
+        device = -1
+    current = _one_gpu(what, device)
+    if rows and heads:
+        cfg = _pack(what, _DENSE, rows, keys[0], q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head, sequences, heads, keys[1], dim,
+                    kind, JENGA_DENSE_CAUSAL if causal else 0, dim ** -0.5 if scale is None else scale, 0)
         # without keys there is nothing to read, but the call wants addresses
         here = q.data_ptr()
-        _check(_lib.jenga_dense_attn(cfg, here, k.data_ptr() or here, v.data_ptr() or here, q_start.data_ptr(), kv_start.data_ptr(),
-                                     None if kv_len is None else kv_len.data_ptr(), out.data_ptr(), workspace.data_ptr(),
-                                     workspace.numel() * workspace.element_size(), stream), what)
+        status = _lib.jenga_dense_attn(cfg, here, k.data_ptr() or here, v.data_ptr() or here, q_start.data_ptr(), kv_start.data_ptr(), at_len,
+                                       out.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                       current if stream is None else stream)
+        if status:
+            raise JengaError(status, what)
 
 
 def make_rotary(T, H, W, head_dim, dims, theta=10000.0, origin=(0.0, 0.0, 0.0), step=(1.0, 1.0, 1.0), flags=0):
