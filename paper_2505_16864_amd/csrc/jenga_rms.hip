@@ -15,6 +15,8 @@ namespace {
 
 using namespace jenga;
 
+enum Out { SAME, EIGHT_BITS, FOUR_BITS };
+
 struct Strided {
   void* at;
   int64_t row, head;
@@ -31,7 +33,6 @@ struct RmsArgs {
   float eps, w0;
 };
 
-enum Out { SAME, EIGHT_BITS, FOUR_BITS };
 
 // Row n of a tensor; n / heads by multiplication, exact below 2^31.
 struct Place {
@@ -48,20 +49,36 @@ __device__ __forceinline__ X* row_of(const Strided& t, const Place& p) {
   return (X*)t.at + p.row * t.row + (int64_t)p.head * t.head;
 }
 
-// Eight values from column `col` on; zeros past the row's end.  `whole`: the same for all lanes, no piece of them is cut.
+// Rows are taken in pieces of eight columns.  Where their number is no multiple of eight, the last piece ends with the row and overlaps the one
+// before it: both compute and store the same results there, and sums take only what is a piece's own.  Nothing of a row is stored before all of
+// it has been read, by whichever wavefront.  Results of few bits have their places in blocks: there, and in rows of less than eight columns,
+// the last piece is read and written one by one (40000 x 2500 bf16: one by one 199 us, its gradient 328; so 164 and 164).
+enum Ends { EVEN, OVER, ONE_BY_ONE };
+struct Piece {
+  int col, skip;   // of the first value; so many are the piece's before
+};
+template <Out OUT>
+__device__ __forceinline__ Ends ends_of(int cols) {
+  return cols % 8 == 0 ? EVEN : OUT == SAME && cols > 8 ? OVER : ONE_BY_ONE;
+}
+__device__ __forceinline__ Piece piece_at(int col, int cols, Ends ends) {
+  const int c = ends == OVER ? min(col, cols - 8) : col;
+  return {c, col - c};
+}
+// Zeros past the row's end.
 template <typename T>
-__device__ __forceinline__ typename Eight<T>::raw piece(const T* p, int col, int cols, bool whole) {
+__device__ __forceinline__ typename Eight<T>::raw piece(const T* p, int col, int cols, Ends ends) {
   typename Eight<T>::raw r = {};
-  if (whole) {
-    if (col < cols) r = *(const typename Eight<T>::raw*)(p + col);
+  if (ends != ONE_BY_ONE) {
+    if (col < cols) r = *(const typename Eight<T>::raw*)(p + piece_at(col, cols, ends).col);
     return r;
   }
   return load_eight(p + col, cols - col);
 }
 template <typename T>
-__device__ __forceinline__ void put_piece(T* p, int col, int cols, bool whole, const f32x8& f) {
-  if (whole) {
-    if (col < cols) *(typename Eight<T>::raw*)(p + col) = Eight<T>::narrow(f);
+__device__ __forceinline__ void put_piece(T* p, int col, int cols, Ends ends, const f32x8& f) {
+  if (ends != ONE_BY_ONE) {
+    if (col < cols) *(typename Eight<T>::raw*)(p + piece_at(col, cols, ends).col) = Eight<T>::narrow(f);
     return;
   }
   store_eight(p + col, f, cols - col);
@@ -94,9 +111,9 @@ __device__ __forceinline__ float lanes_sum(float v, float* room) {
 
 // Eight results of a row from column `col` on; in 8 bits 16 lanes hold a block of 128 columns, in 4 bits four lanes one of 32.
 template <typename X, Out OUT>
-__device__ __forceinline__ void put(const RmsArgs& a, const Place& p, int col, bool whole, bool mine, f32x8 y) {
+__device__ __forceinline__ void put(const RmsArgs& a, const Place& p, int col, Ends ends, bool mine, f32x8 y) {
   if constexpr (OUT == SAME) {
-    if (mine) put_piece(row_of<X>(a.y, p), col, a.cols, whole, y);
+    if (mine) put_piece(row_of<X>(a.y, p), col, a.cols, ends, y);
     return;
   }
 #pragma unroll
@@ -126,21 +143,24 @@ __device__ __forceinline__ void fill_scales(const RmsArgs& a, const Place& p, in
   if (block < a.scale_cols) a.y_scale[p.row * a.scale_cols + block] = 0;
 }
 
-constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
+constexpr int threads_of(int lanes) { return lanes > 128 ? lanes : 256; }
 
-// LANES threads to a row, NV pieces of eight columns each.  A workgroup takes rows a grid apart; it keeps the weight in registers, and the next row
+// LANES threads to a row, NV pieces of eight columns each.  33272 x 5120 bf16 with residual and sum 266 us, 5.1 TB/s (a plain copy: 4.88);
+// Q and K of 33272 x 40 x 128 @.  A workgroup takes rows a grid apart; it keeps the weight in registers, and the next row
 // is on its way while one is worked on.
 template <typename X, typename P, Out OUT, int LANES, int NV>
 __global__ __launch_bounds__(threads_of(LANES)) void rms_kernel(RmsArgs a) {
   constexpr int THREADS = threads_of(LANES), STEP = LANES * 8, AT_ONCE = THREADS / LANES;
   __shared__ float room[2][THREADS / 64];
   const int slot = threadIdx.x / LANES, col0 = threadIdx.x % LANES * 8;
-  const bool even = a.cols % 8 == 0;
+  const Ends ends = ends_of<OUT>(a.cols);
+  // of piece v: one that no row's end is in is an even one
+  auto ends_at = [&](int v) { return v * STEP + STEP <= a.cols ? EVEN : ends; };
   typename Eight<P>::raw weight[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     weight[v] = {};
-    if (a.weight) weight[v] = piece((const P*)a.weight, v * STEP + col0, a.cols, even || v * STEP + STEP <= a.cols);
+    if (a.weight) weight[v] = piece((const P*)a.weight, v * STEP + col0, a.cols, ends_at(v));
   }
   typename Eight<X>::raw next[NV], next_add[NV];
   Place next_place = {};
@@ -152,9 +172,8 @@ __global__ __launch_bounds__(threads_of(LANES)) void rms_kernel(RmsArgs a) {
 #pragma unroll
     for (int v = 0; v < NV; ++v)
       if (v * STEP < a.cols) {
-        const bool whole = even || v * STEP + STEP <= a.cols;
-        next[v] = piece(row_of<X>(a.x, next_place), v * STEP + col0, a.cols, whole);
-        if (a.add.at) next_add[v] = piece(row_of<X>(a.add, next_place), v * STEP + col0, a.cols, whole);
+        next[v] = piece(row_of<X>(a.x, next_place), v * STEP + col0, a.cols, ends_at(v));
+        if (a.add.at) next_add[v] = piece(row_of<X>(a.add, next_place), v * STEP + col0, a.cols, ends_at(v));
       }
   };
   const int64_t step = (int64_t)gridDim.x * AT_ONCE;
@@ -172,9 +191,14 @@ __global__ __launch_bounds__(threads_of(LANES)) void rms_kernel(RmsArgs a) {
       if (v * STEP < a.cols) {
         f[v] = Eight<X>::wide(next[v]);
         if (a.add.at) f[v] = Eight<X>::wide(Eight<X>::narrow(f[v] + Eight<X>::wide(next_add[v])));
-        if (a.sum.at && mine) put_piece(row_of<X>(a.sum, place), v * STEP + col0, a.cols, even || v * STEP + STEP <= a.cols, f[v]);
+        if (ends_at(v) != OVER) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) square = fmaf(f[v][i], f[v][i], square);
+          for (int i = 0; i < 8; ++i) square = fmaf(f[v][i], f[v][i], square);
+        } else {
+          const int skip = piece_at(v * STEP + col0, a.cols, OVER).skip;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) square = fmaf(f[v][i], i >= skip ? f[v][i] : 0.f, square);
+        }
       }
     fetch(row + step);
     const float rstd = 1.0f / sqrtf(lanes_sum<LANES>(square, room[turn]) / (float)a.cols + a.eps);
@@ -186,7 +210,8 @@ __global__ __launch_bounds__(threads_of(LANES)) void rms_kernel(RmsArgs a) {
         f32x8 y;
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = f[v][i] * rstd * w[i];
-        put<X, OUT>(a, place, v * STEP + col0, even || v * STEP + STEP <= a.cols, mine, y);
+        if (a.sum.at && mine) put_piece(row_of<X>(a.sum, place), v * STEP + col0, a.cols, ends_at(v), f[v]);
+        put<X, OUT>(a, place, v * STEP + col0, ends_at(v), mine, y);
       }
     if (OUT == EIGHT_BITS && mine) fill_scales(a, place, threadIdx.x % LANES);
   }
@@ -231,7 +256,7 @@ __global__ __launch_bounds__(1024) void rms_long_kernel(RmsArgs a) {
         if (a.weight) w += Eight<P>::wide(load_eight((const P*)a.weight + col, a.cols - col));
         y = f * rstd * w;
       }
-      put<X, OUT>(a, p, col, false, true, y);
+      put<X, OUT>(a, p, col, ONE_BY_ONE, true, y);
     }
     if (OUT == EIGHT_BITS) fill_scales(a, p, threadIdx.x);
   }
@@ -246,14 +271,15 @@ __global__ __launch_bounds__(threads_of(LANES)) void rms_grad_kernel(RmsArgs a) 
   __shared__ float room[2][THREADS / 64];
   __shared__ float sums[AT_ONCE > 1 ? AT_ONCE * STEP * NV : 1];
   const int slot = threadIdx.x / LANES, col0 = threadIdx.x % LANES * 8;
-  const bool even = a.cols % 8 == 0;
+  const Ends ends = ends_of<SAME>(a.cols);
+  auto ends_at = [&](int v) { return v * STEP + STEP <= a.cols ? EVEN : ends; };
   typename Eight<P>::raw weight[NV];
   f32x8 dw[NV];
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     dw[v] = 0.f;
     weight[v] = {};
-    if (a.weight) weight[v] = piece((const P*)a.weight, v * STEP + col0, a.cols, even || v * STEP + STEP <= a.cols);
+    if (a.weight) weight[v] = piece((const P*)a.weight, v * STEP + col0, a.cols, ends_at(v));
   }
   typename Eight<X>::raw next_s[NV], next_d[NV], next_t[NV];
   float next_r = 0.f;
@@ -269,10 +295,9 @@ __global__ __launch_bounds__(threads_of(LANES)) void rms_grad_kernel(RmsArgs a) 
     for (int v = 0; v < NV; ++v)
       if (v * STEP < a.cols) {
         const int col = v * STEP + col0;
-        const bool whole = even || v * STEP + STEP <= a.cols;
-        next_s[v] = piece(row_of<X>(a.x, next_place), col, a.cols, whole);
-        next_d[v] = piece(row_of<X>(a.y, next_place), col, a.cols, whole);
-        if (a.add.at) next_t[v] = piece(row_of<X>(a.add, next_place), col, a.cols, whole);
+        next_s[v] = piece(row_of<X>(a.x, next_place), col, a.cols, ends_at(v));
+        next_d[v] = piece(row_of<X>(a.y, next_place), col, a.cols, ends_at(v));
+        if (a.add.at) next_t[v] = piece(row_of<X>(a.add, next_place), col, a.cols, ends_at(v));
       }
   };
   const int64_t step = (int64_t)gridDim.x * AT_ONCE;
@@ -291,13 +316,19 @@ __global__ __launch_bounds__(threads_of(LANES)) void rms_grad_kernel(RmsArgs a) 
       if (v * STEP < a.cols) {
         const f32x8 s = Eight<X>::wide(next_s[v]), d = Eight<X>::wide(next_d[v]), w = Eight<P>::wide(weight[v]) + a.w0;
         t[v] = next_t[v];
-        const float r = even && v * STEP + col0 >= a.cols ? 0.f : rstd;   // r may be infinite, and 0 times that is NaN
+        // it is there: dx may go over it
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(t[v]) / 4; ++i) asm volatile("" : "+v"(t[v].w[i]));
+        // rstd may be infinite, and 0 times that is NaN: columns that are not there have h = 0.  Of a piece's before, the sums take nothing
+        const int col = v * STEP + col0, skip = piece_at(col, a.cols, ends_at(v)).skip;
+        const float r = col < a.cols ? rstd : 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          h[v][i] = s[i] * (even || v * STEP + col0 + i < a.cols ? r : 0.f);
+          h[v][i] = s[i] * r;
+          if (ends_at(v) == ONE_BY_ONE && col + i >= a.cols) h[v][i] = 0.f;
           g[v][i] = d[i] * w[i];
           dw[v][i] = fmaf(d[i], h[v][i], dw[v][i]);
-          sum = fmaf(g[v][i], h[v][i], sum);
+          sum = fmaf(i >= skip ? g[v][i] : 0.f, h[v][i], sum);
         }
       }
     fetch(row + step);
@@ -309,19 +340,24 @@ __global__ __launch_bounds__(threads_of(LANES)) void rms_grad_kernel(RmsArgs a) 
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = rstd * fmaf(-h[v][i], mean, g[v][i]);
         if (a.add.at) d += Eight<X>::wide(t[v]);
-        put_piece(row_of<X>(a.sum, place), v * STEP + col0, a.cols, even || v * STEP + STEP <= a.cols, d);
+        put_piece(row_of<X>(a.sum, place), v * STEP + col0, a.cols, ends_at(v), d);
       }
   }
   if (!a.parts) return;
   float* to = a.parts + (int64_t)blockIdx.x * a.cols;
-  if constexpr (AT_ONCE == 1) {
+  // a piece's own columns: to memory, or to LDS where several rows at a time have sums
 #pragma unroll
-    for (int v = 0; v < NV; ++v) store_eight(to + v * STEP + col0, dw[v], a.cols - v * STEP - col0);
-  } else {
+  for (int v = 0; v < NV; ++v) {
+    const int col = v * STEP + col0;
+    const Piece p = piece_at(col, a.cols, ends_at(v));
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sums[slot * STEP * NV + v * STEP + col0 + i] = dw[v][i];
+    for (int i = 0; i < 8; ++i)
+      if (col < a.cols && i >= p.skip && p.col + i < a.cols) {
+        if constexpr (AT_ONCE == 1) to[p.col + i] = dw[v][i];
+        else sums[slot * STEP * NV + p.col + i] = dw[v][i];
+      }
+  }
+  if constexpr (AT_ONCE > 1) {
     __syncthreads();
     for (int col = threadIdx.x; col < a.cols; col += THREADS) {
       float s = 0.f;
@@ -430,7 +466,7 @@ int run_rms(const RmsArgs& a, hipStream_t st) {
   else if (a.cols <= 1536) run_rows<X, P, OUT, 64, 3>(a, st);
   else if (a.cols <= 2048) run_rows<X, P, OUT, 256, 1>(a, st);
   else if (a.cols <= 4096) run_rows<X, P, OUT, 256, 2>(a, st);
-  else if (a.cols <= 6144) run_rows<X, P, OUT, 256, 3>(a, st);
+  else if (a.cols <= 6144) run_rows<X, P, OUT, 768, 1>(a, st);
   else if (a.cols <= 8192) run_rows<X, P, OUT, 512, 2>(a, st);
   else if (a.cols <= 12288) run_rows<X, P, OUT, 512, 3>(a, st);
   else run_rows<X, P, OUT, 1024, 2>(a, st);
@@ -447,10 +483,14 @@ int run_grad_rows(const RmsArgs& a, hipStream_t st) {
   return (int)n;
 }
 
+// One piece a thread where rows have exact shapes for it: gradient of 63424 x 1536 bf16 in three pieces of a wavefront 225 us, in one of
+// three 158; 33272 x 5120 510 -> 266, 12000 x 8192 234 -> 146.  (The forward pass does not mind: 150 and 178 at 1536.)  The last two shapes keep 10 to 21
+// registers in scratch, and still beat the kernel that reads rows again: 6000 x 10000 float32 304 and 337, 6000 x 16000 bf16 228 and 348
+// (4000 x 16000 float32, with 68, does not: 414 and 335).
 template <typename X, typename P>
 int run_grad(const RmsArgs& a, float* dweight, hipStream_t st) {
   int parts;
-  if (a.cols > MOST_COLS) {
+  if (a.cols > (sizeof(X) == 4 ? 12288 : MOST_COLS)) {
     rms_grad_long_kernel<X, P><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), 1024, 0, st>>>(a);
     parts = (int)std::min<int64_t>((a.rows + 7) / 8, 64);
     if (a.parts) rms_grad_columns_kernel<X><<<dim3(parts, (a.cols + 255) / 256), 256, 0, st>>>(a);
@@ -459,10 +499,14 @@ int run_grad(const RmsArgs& a, float* dweight, hipStream_t st) {
   else if (a.cols <= 256) parts = run_grad_rows<X, P, 32, 1>(a, st);
   else if (a.cols <= 512) parts = run_grad_rows<X, P, 64, 1>(a, st);
   else if (a.cols <= 1024) parts = run_grad_rows<X, P, 128, 1>(a, st);
-  else if (a.cols <= 1536) parts = run_grad_rows<X, P, 64, 3>(a, st);
+  else if (a.cols <= 1536) parts = run_grad_rows<X, P, 192, 1>(a, st);
   else if (a.cols <= 2048) parts = run_grad_rows<X, P, 256, 1>(a, st);
-  else if (a.cols <= 4096) parts = run_grad_rows<X, P, 256, 2>(a, st);
-  else if (a.cols <= 8192) parts = run_grad_rows<X, P, 512, 2>(a, st);
+  else if (a.cols <= 3072) parts = run_grad_rows<X, P, 256, 2>(a, st);
+  else if (a.cols <= 4096) parts = run_grad_rows<X, P, 512, 1>(a, st);
+  else if (a.cols <= 5120) parts = run_grad_rows<X, P, 640, 1>(a, st);
+  else if (a.cols <= 6144) parts = run_grad_rows<X, P, 768, 1>(a, st);
+  else if (a.cols <= 8192) parts = run_grad_rows<X, P, 1024, 1>(a, st);
+  else if (a.cols <= 12288) parts = run_grad_rows<X, P, 768, 2>(a, st);
   else parts = run_grad_rows<X, P, 1024, 2>(a, st);
   if (a.parts) rms_grad_sum_kernel<<<(a.cols + 31) / 32, 1024, 0, st>>>(a.parts, dweight, a.cols, parts);
   return status();
