@@ -10,6 +10,7 @@
 
 #include "jenga_device.h"
 #include "jenga_internal.h"
+#include "jenga_tiles.h"
 
 namespace {
 
@@ -31,6 +32,9 @@ struct RmsArgs {
   uint32_t heads, by_heads, heads_shift;
   int32_t cols, scale_cols, y_bytes;
   float eps, w0;
+  // Results of 16 bits of more than 64 MiB go past the caches: 33272 x 5120 267 -> 262 us, gradient 268 -> 255; 60000 x 1024 99 -> 79; Q and K of
+  // 33272 x 40 x 128 160 -> 148 each.  (Smaller ones may be read again from there; float32 rows off the 16-byte grid lose, 12068 x 777 24 -> 31.)
+  bool past;
 };
 
 
@@ -75,10 +79,20 @@ __device__ __forceinline__ typename Eight<T>::raw piece(const T* p, int col, int
   }
   return load_eight(p + col, cols - col);
 }
+// past: not to be kept in the caches.
 template <typename T>
-__device__ __forceinline__ void put_piece(T* p, int col, int cols, Ends ends, const f32x8& f) {
+__device__ __forceinline__ void put_piece(T* p, int col, int cols, Ends ends, bool past, const f32x8& f) {
   if (ends != ONE_BY_ONE) {
-    if (col < cols) *(typename Eight<T>::raw*)(p + piece_at(col, cols, ends).col) = Eight<T>::narrow(f);
+    if (col >= cols) return;
+    T* to = p + piece_at(col, cols, ends).col;
+    const auto r = Eight<T>::narrow(f);
+    if constexpr (sizeof(T) == 2) {
+      if (past) {
+        store_once(to, make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
+        return;
+      }
+    }
+    *(typename Eight<T>::raw*)to = r;
     return;
   }
   store_eight(p + col, f, cols - col);
@@ -113,7 +127,7 @@ __device__ __forceinline__ float lanes_sum(float v, float* room) {
 template <typename X, Out OUT>
 __device__ __forceinline__ void put(const RmsArgs& a, const Place& p, int col, Ends ends, bool mine, f32x8 y) {
   if constexpr (OUT == SAME) {
-    if (mine) put_piece(row_of<X>(a.y, p), col, a.cols, ends, y);
+    if (mine) put_piece(row_of<X>(a.y, p), col, a.cols, ends, a.past, y);
     return;
   }
 #pragma unroll
@@ -145,8 +159,8 @@ __device__ __forceinline__ void fill_scales(const RmsArgs& a, const Place& p, in
 
 constexpr int threads_of(int lanes) { return lanes > 128 ? lanes : 256; }
 
-// LANES threads to a row, NV pieces of eight columns each.  33272 x 5120 bf16 with residual and sum 266 us, 5.1 TB/s (a plain copy: 4.88);
-// Q and K of 33272 x 40 x 128 @.  A workgroup takes rows a grid apart; it keeps the weight in registers, and the next row
+// LANES threads to a row, NV pieces of eight columns each.  33272 x 5120 bf16 with residual and sum 262 us, 5.2 TB/s (a plain copy: 4.88);
+// Q and K of 33272 x 40 x 128 148 each, 4.6 TB/s out of a projection's rows.  A workgroup takes rows a grid apart; it keeps the weight in registers, and the next row
 // is on its way while one is worked on.
 template <typename X, typename P, Out OUT, int LANES, int NV>
 __global__ __launch_bounds__(threads_of(LANES)) void rms_kernel(RmsArgs a) {
@@ -210,7 +224,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void rms_kernel(RmsArgs a) {
         f32x8 y;
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = f[v][i] * rstd * w[i];
-        if (a.sum.at && mine) put_piece(row_of<X>(a.sum, place), v * STEP + col0, a.cols, ends_at(v), f[v]);
+        if (a.sum.at && mine) put_piece(row_of<X>(a.sum, place), v * STEP + col0, a.cols, ends_at(v), a.past, f[v]);
         put<X, OUT>(a, place, v * STEP + col0, ends_at(v), mine, y);
       }
     if (OUT == EIGHT_BITS && mine) fill_scales(a, place, threadIdx.x % LANES);
@@ -340,7 +354,7 @@ __global__ __launch_bounds__(threads_of(LANES)) void rms_grad_kernel(RmsArgs a) 
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = rstd * fmaf(-h[v][i], mean, g[v][i]);
         if (a.add.at) d += Eight<X>::wide(t[v]);
-        put_piece(row_of<X>(a.sum, place), v * STEP + col0, a.cols, ends_at(v), d);
+        put_piece(row_of<X>(a.sum, place), v * STEP + col0, a.cols, ends_at(v), a.past, d);
       }
   }
   if (!a.parts) return;
@@ -507,7 +521,8 @@ int run_grad(const RmsArgs& a, float* dweight, hipStream_t st) {
   else if (a.cols <= 6144) parts = run_grad_rows<X, P, 768, 1>(a, st);
   else if (a.cols <= 8192) parts = run_grad_rows<X, P, 1024, 1>(a, st);
   else if (a.cols <= 12288) parts = run_grad_rows<X, P, 768, 2>(a, st);
-  else parts = run_grad_rows<X, P, 1024, 2>(a, st);
+  else if constexpr (sizeof(X) == 2) parts = run_grad_rows<X, P, 1024, 2>(a, st);
+  else return JENGA_EUNSUPPORTED;   // not reached
   if (a.parts) rms_grad_sum_kernel<<<(a.cols + 31) / 32, 1024, 0, st>>>(a.parts, dweight, a.cols, parts);
   return status();
 }
@@ -532,6 +547,7 @@ RmsArgs args_of(const jenga_rms_config& c) {
   a.scale_cols = c.y_type == JENGA_E4M3 ? (blocks + 3) / 4 * 4 : blocks * 4;
   a.eps = c.eps;
   a.w0 = c.weight_offset;
+  a.past = (double)a.rows * c.cols * 2 > 64.0 * (1 << 20);
   return a;
 }
 

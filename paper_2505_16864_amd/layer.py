@@ -97,11 +97,13 @@ class CarveLayer:
 
 class CarveBlock:
     """The attention half of a transformer block on hidden states: a modulated layer norm straight to 8 bits, one 8-bit product for Q, K
-    and V, a CarveLayer with rotary positions, an 8-bit output projection.  Owns the weights in 8 bits and every buffer."""
+    and V, a norm of Q and K where they have one, a CarveLayer with rotary positions, an 8-bit output projection.  Owns the weights in 8 bits
+    and every buffer."""
 
-    def __init__(self, w, w_qkv, b_qkv, w_out, b_out, rotary, device="cuda:0", eps=1e-6, **layer):
+    def __init__(self, w, w_qkv, b_qkv, w_out, b_out, rotary, device="cuda:0", eps=1e-6, qk_norm=None, **layer):
         """w: a workload of CarveLayer.  w_qkv [3 * heads * head_dim, hidden] (rows of Q, K, V), w_out [hidden, heads * head_dim] in
-        bf16, fp16 or float32; b_qkv, b_out float32 or None.  rotary and **layer: of CarveLayer."""
+        bf16, fp16 or float32; b_qkv, b_out float32 or None.  qk_norm: None, or the weights [head_dim] of the root-mean-square norms of
+        each head of Q and of K, bf16 or float32.  rotary and **layer: of CarveLayer."""
         inner, hidden = w["heads"] * w["head_dim"], w_out.shape[0]
         if tuple(w_qkv.shape) != (3 * inner, hidden) or w_out.shape[1] != inner:
             raise ValueError("weights of shapes %s and %s for %d heads x %d" % (tuple(w_qkv.shape), tuple(w_out.shape), w["heads"],
@@ -117,6 +119,7 @@ class CarveBlock:
             self.w_qkv, self.s_qkv = self._quantized(w_qkv.to(dev), 128)
             self.w_out, self.s_out = self._quantized(w_out.to(dev), 128)
             self.b_qkv, self.b_out = [None if b is None else b.to(dev, torch.float32).contiguous() for b in (b_qkv, b_out)]
+            self.qk_norm = None if qk_norm is None else [n.to(dev).contiguous() for n in qk_norm]
             self.x, self.s_x = self._room(rows, hidden)
             self.o, self.s_o = self._room(rows, inner)
             self.qkv = torch.empty((self.batch, self.tokens, 3, w["heads"], w["head_dim"]), dtype=torch.bfloat16, device=dev)
@@ -138,6 +141,10 @@ class CarveBlock:
         B.jenga_layer_norm(x.reshape(-1, self.hidden), self.x, scale, shift, y_scale=self.s_x, group_rows=self.tokens, weight_offset=1.0,
                            eps=self.eps, stream=stream)
         B.jenga_matmul(self.x, self.s_x, self.w_qkv, self.s_qkv, self.qkv.view(-1, self.w_qkv.shape[0]), self.b_qkv, stream=stream)
+        if self.qk_norm is not None:
+            for i, weight in enumerate(self.qk_norm):
+                t = self.qkv.flatten(0, 1)[:, i]
+                B.jenga_rms_norm(t, t, weight, eps=self.eps, stream=stream)
         return self.qkv.unbind(2)
 
     def forward(self, x, scale=None, shift=None):
@@ -150,3 +157,74 @@ class CarveBlock:
 
     def close(self):
         self.layer.close()
+
+
+class DenseBlock:
+    """The attention half of a transformer block on packed sequences, in 4 bits: the addition of a residual and a root-mean-square norm straight to
+    4 bits, one 4-bit product for Q, K and V, norms of each head of Q and K, rotary positions, attention to all keys with heads that share
+    them, a 4-bit output projection.  Owns the weights in 4 bits and every buffer, for `rows` rows in `sequences` sequences at most."""
+
+    def __init__(self, rows, sequences, heads, kv_heads, head_dim, w_qkv, b_qkv, w_out, b_out, norm, qk_norm=None, rotary=None, causal=True,
+                 device="cuda:0", eps=1e-6):
+        """w_qkv [(heads + 2 * kv_heads) * head_dim, hidden] (rows of Q, K, V), w_out [hidden, heads * head_dim] in bf16, fp16 or float32; b_qkv,
+        b_out float32 or None; norm [hidden], qk_norm None or two of [head_dim], bf16 or float32.  rotary: None, or the arguments of
+        make_rotary() by name, T, H, W, dims and others, head_dim excepted."""
+        inner, hidden, width = heads * head_dim, w_out.shape[0], (heads + 2 * kv_heads) * head_dim
+        if tuple(w_qkv.shape) != (width, hidden) or w_out.shape[1] != inner or tuple(norm.shape) != (hidden,):
+            raise ValueError("weights of shapes %s, %s and %s for %d heads, %d of keys, x %d" % (
+                tuple(w_qkv.shape), tuple(w_out.shape), tuple(norm.shape), heads, kv_heads, head_dim))
+        self.device, self.eps, self.causal = torch.device(device), eps, causal
+        self.heads, self.kv_heads, self.head_dim, self.hidden, self.inner, self.rows, self.sequences = (heads, kv_heads, head_dim, hidden, inner,
+                                                                                                         rows, sequences)
+        dev = self.device
+        with torch.cuda.device(dev):
+            self.w_qkv, self.s_qkv = self._quantized(w_qkv.to(dev))
+            self.w_out, self.s_out = self._quantized(w_out.to(dev))
+            self.b_qkv, self.b_out = [None if b is None else b.to(dev, torch.float32).contiguous() for b in (b_qkv, b_out)]
+            self.norm = norm.to(dev).contiguous()
+            self.qk_norm = None if qk_norm is None else [n.to(dev).contiguous() for n in qk_norm]
+            self.rotary = None
+            if rotary is not None:
+                self.rotary = B.make_rotary(head_dim=head_dim, **rotary)
+                table = torch.empty(sum(n * d for n, d in zip((self.rotary.T, self.rotary.H, self.rotary.W), self.rotary.dim)), dtype=torch.float32)
+                B.jenga_rotary_table(self.rotary, table)
+                self.rotary_table = table.to(dev)
+            self.x, self.s_x = self._room(rows, hidden)
+            self.o, self.s_o = self._room(rows, inner)
+            self.total, self.out = [torch.empty((rows, hidden), dtype=torch.bfloat16, device=dev) for _ in range(2)]
+            self.qkv = torch.empty((rows, heads + 2 * kv_heads, head_dim), dtype=torch.bfloat16, device=dev)
+            self.attended = torch.empty((rows, heads, head_dim), dtype=torch.bfloat16, device=dev)
+            self.room = torch.empty(B.jenga_dense_attn_workspace(rows, rows, sequences, heads, kv_heads, head_dim), dtype=torch.uint8, device=dev)
+
+    def _room(self, rows, cols):
+        padded = B.padded_columns(cols)
+        return (torch.empty((rows, padded // 2), dtype=torch.uint8, device=self.device),
+                torch.empty((rows, padded // 32), dtype=torch.uint8, device=self.device))
+
+    def _quantized(self, weight):
+        q, scale = self._room(*weight.shape)
+        B.jenga_quantize_mx(weight.contiguous(), q, scale)
+        return q, scale
+
+    def forward(self, x, starts, residual=None, cells=None):
+        """x, residual bf16 [n, hidden], starts int32 [sequences + 1] on the device: rows of each sequence; cells int32 [n, 3] where there are
+        rotary positions.  Returns the sum of x and residual and what the block adds to it, bf16 [n, hidden], overwritten by the next
+        call.  All on torch's current stream."""
+        n = x.shape[0]
+        if n > self.rows or starts.numel() - 1 > self.sequences:
+            raise ValueError("%d rows of %d sequences for a block of %d and %d" % (n, starts.numel() - 1, self.rows, self.sequences))
+        if (cells is None) != (self.rotary is None):
+            raise ValueError("cells are wanted where there are rotary positions, and only there")
+        total, out, qkv, attended = self.total[:n], self.out[:n], self.qkv[:n], self.attended[:n]
+        q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
+        B.jenga_rms_norm(x, self.x[:n], self.norm, residual=residual, total=total, y_scale=self.s_x[:n], eps=self.eps)
+        B.jenga_matmul_mx(self.x[:n], self.s_x[:n], self.w_qkv, self.s_qkv, qkv.view(n, -1), self.b_qkv)
+        if self.qk_norm is not None:
+            for t, weight in zip((q, k), self.qk_norm):
+                B.jenga_rms_norm(t, t, weight, eps=self.eps)
+        if self.rotary is not None:
+            B.jenga_rotary(self.rotary, self.rotary_table, q[None], q[None], k[None], k[None], cells=cells[None])
+        B.jenga_dense_attn(q, k, v, attended, starts, starts, causal=self.causal, workspace=self.room)
+        B.jenga_quantize_mx(attended.view(n, self.inner), self.o[:n], self.s_o[:n])
+        B.jenga_matmul_mx(self.o[:n], self.s_o[:n], self.w_out, self.s_out, out, self.b_out)
+        return total, out
