@@ -92,7 +92,21 @@ MatmulTiles matmul_tiles(int64_t m, int64_t n, bool float32) {
   return {0, 128, 128, 2, 2};
 }
 
-MatmulTiles matmul_mx_tiles(int64_t m, int64_t n) { return matmul_tiles(m, n, false); }
+// The same for 4-bit operands, whose products take half the time, so that a tile's start and end weigh more: a round of tiles of 256 x 256 takes
+// 1.6 times as long as one of 128 x 128 at k of 8192, 1.7 to 1.77 at 4096 and 5120, 2 to 2.2 at 1536, 2.5 at 512.  256 -> 128, us, by rounds of either: 31 and 62, 33272 x
+// 15360 x 5120 1403 -> 1740; 1 and 2, 2048 x 5120 x 5120 40.2 -> 45.6; 3 and 5, 9000 x 4000 x 4096 108 -> 102, 7000 x 5000 x 5120 132 -> 124; 4 and 7, 11264 x 4608 x
+// 1536 75.0 -> 59.8; 2 and 4, 25000 x 1024 x 512 24.7 -> 19.9; 1 and 2, 600 x 16000 x 1024 17.9 -> 13.4.  Float32 results, twice the stores: 9 and 18, 31712 x 4608 x
+// 1536 215 -> 195; 31 and 62, 33272 x 15360 x 5120 1612 -> 1992.
+MatmulTiles matmul_mx_tiles(int64_t m, int64_t n, int64_t k, bool float32) {
+  auto rounds = [&](int size, int at_once) {
+    const int64_t tiles = (m + size - 1) / size * ((n + size - 1) / size);
+    return (double)((tiles + at_once - 1) / at_once);
+  };
+  const MatmulTiles small = matmul_tiles(m, n, true);
+  if (small.rows || small.stages == 4) return small;
+  const double longer = float32 ? 1.8 + 500.0 / (double)k : 1.7 + 400.0 / (double)k;
+  return longer * rounds(256, 256) <= rounds(128, 512) ? MatmulTiles{0, 256, 256, 2, 1} : small;
+}
 
 // ---- arguments of the calls around the attention
 

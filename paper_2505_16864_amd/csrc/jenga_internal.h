@@ -197,7 +197,7 @@ struct MatmulTiles {
   int per_cu;               // workgroups on a compute unit
 };
 MatmulTiles matmul_tiles(int64_t m, int64_t n, bool float32);
-MatmulTiles matmul_mx_tiles(int64_t m, int64_t n);   // of 4-bit operands
+MatmulTiles matmul_mx_tiles(int64_t m, int64_t n, int64_t k, bool float32);   // of 4-bit operands
 
 // Dense attention.  The rows of a sequence and of the heads that share keys are packed, row n is token n / group, head n % group, and cut
 // into tiles of `rows` rows.  Lengths are on the device; the host knows bounds of what there is to do.

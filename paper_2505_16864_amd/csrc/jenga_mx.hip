@@ -406,7 +406,7 @@ int run_rows(const MatmulArgs& g, hipStream_t st) {
 
 template <typename O>
 int run_matmul(const MatmulArgs& g, hipStream_t st) {
-  const jenga::MatmulTiles t = jenga::matmul_mx_tiles(g.m, g.n);
+  const jenga::MatmulTiles t = jenga::matmul_mx_tiles(g.m, g.n, g.halves * 128, sizeof(O) == 4);
   if (t.rows == 16) return run_rows<O, 1>(g, st);
   if (t.rows == 32) return run_rows<O, 2>(g, st);
   if (g.halves < 4) return run_tiles<O, 64, 128, 4, true>(g, 1, st);
