@@ -597,7 +597,9 @@ int dense_args_ok(const jenga_dense_config* c, const void* q, const void* k, con
 DenseShape dense_shape(const jenga_dense_config& c) {
   DenseShape s;
   const int64_t group = c.heads / c.kv_heads, rows = c.q_rows * group;
-  s.rows = rows <= 32 * (int64_t)c.sequences ? 16 : 128;
+// Tiles of 16 rows for a few tokens each: 16 sequences of 3 tokens over 4000 keys x 8 heads 56 us, in tiles of 128 76; 64 x 4 tokens, four heads on one of
+  // keys, 59 and 58; 64 x 20 tokens 130 and 101.  Few tokens on average may be a long prompt and many single tokens: 8000 and 300 x 1, 16 heads, 1353 and 685.
+  s.rows = c.q_rows <= 4 * (int64_t)c.sequences && rows <= 32 * (int64_t)c.sequences ? 16 : 128;
   s.workgroups = s.rows == 16 ? 512 : c.head_dim == 128 ? 768 : 1024;   // that the chip holds, or that keep its memory busy
   // each sequence ends with a tile that may not be full
   s.tiles = rows == 0 ? 0 : rows / s.rows + c.sequences;

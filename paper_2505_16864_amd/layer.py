@@ -218,7 +218,7 @@ class DenseBlock:
         total, out, qkv, attended = self.total[:n], self.out[:n], self.qkv[:n], self.attended[:n]
         q, k, v = qkv.split([self.heads, self.kv_heads, self.kv_heads], dim=1)
         B.jenga_rms_norm(x, self.x[:n], self.norm, residual=residual, total=total, y_scale=self.s_x[:n], eps=self.eps)
-        B.jenga_matmul_mx(self.x[:n], self.s_x[:n], self.w_qkv, self.s_qkv, qkv.view(n, -1), self.b_qkv)
+        B.jenga_matmul_mx(self.x[:n], self.s_x[:n], self.w_qkv, self.s_qkv, qkv.view(n, self.w_qkv.shape[0]), self.b_qkv)
         if self.qk_norm is not None:
             for t, weight in zip((q, k), self.qk_norm):
                 B.jenga_rms_norm(t, t, weight, eps=self.eps)

@@ -98,6 +98,8 @@ def test_dense_block_in_a_graph_and_refusals():
         block.out.zero_()
         want = [t[:200 - 7 * i].clone() for t in block.forward(x, starts)]
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+    total, out = block.forward(x[:0], torch.zeros(1, dtype=torch.int32, device="cuda:0"))
+    assert total.shape == out.shape == (0, 192)
     with pytest.raises(ValueError):
         block.forward(torch.zeros((257, 192), dtype=torch.bfloat16, device="cuda:0"), starts)
     with pytest.raises(ValueError):
