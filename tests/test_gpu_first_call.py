@@ -11,7 +11,7 @@ CODE = """
 import torch
 import paper_2505_16864_amd as J
 t = lambda *shape, dtype=torch.bfloat16: torch.ones(shape, dtype=dtype, device="cuda:0")
-# a byte of 1 is 0.5 in the even column and 0 in the odd one
+# h = 2 / sqrt(4 + 1e-6) is off 1 by 1.3e-7, its float32 sums by 80 * 2^-24 at most; a byte of 1 is 0.5 in the even column and 0 in the odd one
 x, w, y, total, rstd = t(70, 640), t(640), t(70, 640), t(70, 640), t(70, dtype=torch.float32)
 q, s, b, bs, out = t(70, 320, dtype=torch.uint8), t(70, 20, dtype=torch.uint8), t(200, 320, dtype=torch.uint8), t(200, 20, dtype=torch.uint8) * 127, t(70, 200)
 dx, dw, room = t(70, 640), t(640, dtype=torch.float32), t(J.jenga_rms_norm_grad_workspace(70, 640), dtype=torch.uint8)
@@ -28,7 +28,7 @@ with torch.cuda.graph(graph):
 for _ in range(3):
     graph.replay()
     torch.cuda.synchronize()
-assert bool((y == 1).all()) and bool((total == 2).all()) and bool((o == 1).all()) and float(dw[0]) == 70 and bool((out == 320 * 0.5).all()), (y, o, dw, out)
+assert bool((y == 1).all()) and bool((total == 2).all()) and bool((o == 1).all()) and bool(((dw - 70).abs() < 70 * 6e-6).all()) and bool((out == 320 * 0.5).all()), (y, o, dw, out)
 print("as eager calls")
 """
 
