@@ -515,7 +515,7 @@ int run_grad(const RmsArgs& a, float* dweight, hipStream_t st) {
   else if (a.cols <= 1024) parts = run_grad_rows<X, P, 128, 1>(a, st);
   else if (a.cols <= 1536) parts = run_grad_rows<X, P, 192, 1>(a, st);
   else if (a.cols <= 2048) parts = run_grad_rows<X, P, 256, 1>(a, st);
-  else if (a.cols <= 3072) parts = run_grad_rows<X, P, 256, 2>(a, st);
+  else if (a.cols <= 3584) parts = run_grad_rows<X, P, 256, 2>(a, st);
   else if (a.cols <= 4096) parts = run_grad_rows<X, P, 512, 1>(a, st);
   else if (a.cols <= 5120) parts = run_grad_rows<X, P, 640, 1>(a, st);
   else if (a.cols <= 6144) parts = run_grad_rows<X, P, 768, 1>(a, st);
