@@ -850,7 +850,10 @@ __global__ __launch_bounds__(256) void dense_merge_rows_kernel(DenseArgs a) {
     l = l * alpha + wave_sum_f32(sum * weight);
     o *= alpha;
     const int n = min(64, it.parts - p0);
-    for (int q = group; q < n; q += 4 * GROUPS) {   // four at a time; past the last one it again, and not taken
+    // Four at a time; past the last one it again, and not taken.  The turns are the same for all lanes: a lane that had no part left and was out of the
+    // loop would hand its weight, of a part that another group takes, to nobody.
+    for (int q0 = 0; q0 < n; q0 += 4 * GROUPS) {
+      const int q = q0 + group;
       f32x4 x[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = *(const f32x4*)(a.part + (first + step * (p0 + min(q + i * GROUPS, n - 1))) * D + c);
