@@ -37,7 +37,7 @@ struct DenseArgs {
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
   int32_t q_rows, kv_rows, sequences, kv_heads, group;
   uint32_t by_group, group_shift;
-  int32_t causal;
+  int32_t causal, take_out;   // take_out: steps that some rows do not see whole may hold values of keys that they do not see, or that are not there
   float scale_log2e;
   int32_t tile, keys, max_tiles, max_slots, workgroups, may_split;   // keys: of a step
   int32_t *counts, *bins;   // of a list: items and merges; tiles of the sequences in front of each
@@ -562,7 +562,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(Dens
     }
     l_run += sum;
     landed();
-    if (masked && a.causal) {
+    if (masked && a.take_out) {
 #pragma unroll
       for (int c = 0; c < COPIES; ++c) taken |= take_out<T>(vs_wave + c * 4096 + lane * 16);
     }
@@ -578,7 +578,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(Dens
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul32(__builtin_bit_cast(eight, v_fragment(dt, p)), pb[p], O[dt]);
   }
-  if (a.causal && __syncthreads_or(taken)) {   // what was taken out, to the rows that see it: it makes of a sum what it is itself
+  if (a.take_out && __syncthreads_or(taken)) {   // what was taken out, to the rows that see it: it makes of a sum what it is itself
     for (int key = it.begin + max(all_see - it.begin, 0) / KEYS * KEYS; key < min(it.end, r.limit); ++key) {
       const T* v = (const T*)v0 + (int64_t)key * a.v_row + 4 * hl;
 #pragma unroll
@@ -700,7 +700,7 @@ __global__ __launch_bounds__(64 * ROWS_WAVES) void dense_rows_kernel(DenseArgs a
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(ALIGNED ? 2 * COPIES : 0) : "memory");
     const uint32_t at = lds + stage * 2 * BYTES;
     const bool masked = key + KEYS > all_see;
-    if (masked && a.causal) {
+    if (masked && a.take_out) {
 #pragma unroll
       for (int c = 0; c < COPIES; ++c) taken |= take_out<T>(at + BYTES + c * 1024 + lane * 16);
     }
@@ -768,7 +768,7 @@ __global__ __launch_bounds__(64 * ROWS_WAVES) void dense_rows_kernel(DenseArgs a
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");   // nothing is on its way into LDS
 
-  if (a.causal && __ballot(taken) != 0) {   // what was taken out, to the rows that see it: it makes of a sum what it is itself
+  if (a.take_out && __ballot(taken) != 0) {   // what was taken out, to the rows that see it: it makes of a sum what it is itself
     for (int step = first_key; step < it.end; step += WAVES * KEYS) {
       if (step + KEYS <= all_see) continue;
       for (int j = step; j < min(min(step + KEYS, it.end), r.limit); ++j) {
@@ -979,6 +979,7 @@ int jenga_dense_attn(const jenga_dense_config* cfg, const void* q, const void* k
   a.group_shift = (uint32_t)l;
   a.by_group = (uint32_t)((((1ull << l) - (uint64_t)a.group) << 32) / (uint64_t)a.group + 1);
   a.causal = (c.flags & JENGA_DENSE_CAUSAL) != 0;
+  a.take_out = a.causal || c.v_row < c.head_dim;   // rows over each other: behind the last key's value lie others, not zeros
   a.scale_log2e = c.scale * 1.4426950408889634f;
   a.tile = s.rows;
   a.keys = s.rows == 16 ? 32 * ROWS_WAVES : 64;
