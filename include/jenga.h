@@ -564,8 +564,12 @@ int jenga_dense_attn(const jenga_dense_config* cfg, const void* q, const void* k
                      const int32_t* kv_start, const int32_t* kv_len_or_null, void* out, void* workspace, size_t workspace_bytes,
                      void* stream);
 
-/* Bytes of its workspace (host only); strides are not looked at. */
+/* Bytes of its workspace (host only), for a call of just these rows and sequences: one with fewer of either may need more, where its keys are cut into parts.
+ * Strides are not looked at. */
 int jenga_dense_attn_workspace(const jenga_dense_config* cfg, uint64_t* bytes);
+
+/* Bytes that are enough for it and for every call with no more rows, keys and sequences (host only): some 200 to 400 MB as a rule. */
+int jenga_dense_attn_workspace_up_to(const jenga_dense_config* cfg, uint64_t* bytes);
 
 /* Static, NUL-terminated description of a status code. */
 const char* jenga_strerror(int status);

@@ -27,7 +27,7 @@ EXPORTS = ["jenga_plan_create", "jenga_plan_destroy", "jenga_plan_info", "jenga_
            "jenga_block_sparse_attn_packed", "jenga_unpermute", "jenga_forward", "jenga_stage_switch",
            "jenga_quantize", "jenga_matmul", "jenga_layer_norm", "jenga_layer_norm_grad", "jenga_layer_norm_grad_workspace",
            "jenga_quantize_mx", "jenga_matmul_mx", "jenga_rms_norm", "jenga_rms_norm_grad", "jenga_rms_norm_grad_workspace",
-           "jenga_dense_attn", "jenga_dense_attn_workspace",
+           "jenga_dense_attn", "jenga_dense_attn_workspace", "jenga_dense_attn_workspace_up_to",
            "jenga_rotary_table", "jenga_rotary", "jenga_forward_rotary", "jenga_strerror"]
 
 
@@ -122,7 +122,7 @@ def _load():
     lib.jenga_rms_norm_grad.argtypes = [vp] * 9 + [size, vp]
     lib.jenga_rms_norm_grad_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
     lib.jenga_dense_attn.argtypes = [vp] * 9 + [size, vp]
-    lib.jenga_dense_attn_workspace.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
+    lib.jenga_dense_attn_workspace.argtypes = lib.jenga_dense_attn_workspace_up_to.argtypes = [vp, ctypes.POINTER(ctypes.c_uint64)]
     lib.jenga_rotary_table.argtypes = [ctypes.POINTER(jenga_rotary_config), vp]
     lib.jenga_rotary.argtypes = [vp] * 5 + [i32, i64, i64, vp]
     lib.jenga_forward_rotary.argtypes = [vp, ctypes.POINTER(jenga_rotary_config)] + [vp] * 4 + [i64] + [vp] * 7 + [size, vp, vp, vp,
@@ -672,13 +672,21 @@ def jenga_rms_norm_grad(total, dy, dx, weight, rstd, dtotal=None, dweight=None, 
             raise JengaError(status, what)
 
 
-def jenga_dense_attn_workspace(q_rows, kv_rows, sequences, heads, kv_heads, head_dim):
-    """Bytes of the workspace of jenga_dense_attn for these numbers of rows, keys and sequences in all."""
+def _dense_bytes(call, q_rows, kv_rows, sequences, heads, kv_heads, head_dim):
     bytes_ = ctypes.c_uint64()
-    cfg = _pack("jenga_dense_attn_workspace", _DENSE, q_rows, kv_rows, 0, 0, 0, 0, 0, 0, 0, 0, sequences, heads, kv_heads, head_dim,
-                JENGA_BF16, 0, 1.0, 0)
-    _check(_lib.jenga_dense_attn_workspace(cfg, ctypes.byref(bytes_)), "jenga_dense_attn_workspace")
+    cfg = _pack(call, _DENSE, q_rows, kv_rows, 0, 0, 0, 0, 0, 0, 0, 0, sequences, heads, kv_heads, head_dim, JENGA_BF16, 0, 1.0, 0)
+    _check(getattr(_lib, call)(cfg, ctypes.byref(bytes_)), call)
     return bytes_.value
+
+
+def jenga_dense_attn_workspace(q_rows, kv_rows, sequences, heads, kv_heads, head_dim):
+    """Bytes of the workspace of jenga_dense_attn for just these numbers of rows, keys and sequences in all; fewer may need more."""
+    return _dense_bytes("jenga_dense_attn_workspace", q_rows, kv_rows, sequences, heads, kv_heads, head_dim)
+
+
+def jenga_dense_attn_workspace_up_to(q_rows, kv_rows, sequences, heads, kv_heads, head_dim):
+    """Bytes that are enough for every call with no more rows, keys and sequences."""
+    return _dense_bytes("jenga_dense_attn_workspace_up_to", q_rows, kv_rows, sequences, heads, kv_heads, head_dim)
 
 
 def jenga_dense_attn(q, k, v, out, q_start, kv_start, kv_len=None, causal=False, scale=None, workspace=None, stream=None):

@@ -548,6 +548,8 @@ int matmul_mx_args_ok(const jenga_matmul_config* c, const void* a, const uint8_t
   return JENGA_OK;
 }
 
+constexpr int64_t DENSE_WORKGROUPS = 1 << 23;   // of a launch, at most
+
 int dense_config_ok(const jenga_dense_config* c) {
   if (!c || c->q_rows < 0 || c->kv_rows < 0 || c->sequences < 0 || c->heads < 1 || c->kv_heads < 1 || c->heads % c->kv_heads != 0 ||
       c->reserved != 0)
@@ -558,7 +560,7 @@ int dense_config_ok(const jenga_dense_config* c) {
   if ((c->head_dim != 64 && c->head_dim != 128) || c->sequences > 1 << 16 || c->heads > 1 << 12) return JENGA_EUNSUPPORTED;
   const int64_t most = (1ll << 31) - 1;
   if (c->q_rows > most || c->kv_rows > most || c->q_rows * (c->heads / c->kv_heads) > most) return JENGA_EUNSUPPORTED;
-  if (dense_shape(*c).items * c->kv_heads > 1 << 23) return JENGA_EUNSUPPORTED;   // workgroups of a launch
+  if (dense_shape(*c).items * c->kv_heads > DENSE_WORKGROUPS) return JENGA_EUNSUPPORTED;
   return JENGA_OK;
 }
 
@@ -594,34 +596,55 @@ int dense_args_ok(const jenga_dense_config* c, const void* q, const void* k, con
   return workspace_bytes < need ? JENGA_EWORKSPACE : JENGA_OK;
 }
 
-DenseShape dense_shape(const jenga_dense_config& c) {
+namespace {
+
+// What a call of `rows` packed rows and so many sequences needs, in tiles of `tile` rows.  Everything here grows with rows and sequences as long as may_split and
+// listed stay as they are, and is largest where tiles may be cut and there is no list.
+DenseShape dense_shape_of(const jenga_dense_config& c, int64_t rows, int64_t sequences, int tile, bool may_split, bool listed) {
   DenseShape s;
-  const int64_t group = c.heads / c.kv_heads, rows = c.q_rows * group;
-// Tiles of 16 rows for a few tokens each: 16 sequences of 3 tokens over 4000 keys x 8 heads 56 us, in tiles of 128 76; 64 x 4 tokens, four heads on one of
-  // keys, 59 and 58; 64 x 20 tokens 130 and 101.  Few tokens on average may be a long prompt and many single tokens: 8000 and 300 x 1, 16 heads, 1353 and 685.
-  s.rows = c.q_rows <= 4 * (int64_t)c.sequences && rows <= 32 * (int64_t)c.sequences ? 16 : 128;
-  s.workgroups = s.rows == 16 ? 512 : c.head_dim == 128 ? 768 : 1024;   // that the chip holds, or that keep its memory busy
+  s.rows = tile;
+  s.may_split = may_split;
+  s.listed = listed;
+  s.workgroups = tile == 16 ? 512 : c.head_dim == 128 ? 768 : 1024;   // that the chip holds, or that keep its memory busy
   // each sequence ends with a tile that may not be full
-  s.tiles = rows == 0 ? 0 : rows / s.rows + c.sequences;
-  // full tiles that there are at least
-  const int64_t least = rows / s.rows;
-  s.may_split = least * c.kv_heads < 2 * s.workgroups;
-  s.listed = c.sequences > 64;
+  s.tiles = rows == 0 ? 0 : rows / tile + sequences;
   // A tile of n steps makes ceil(n / chunk) parts, and a chunk is half of a workgroup's share of the steps at least.  Without a list the tiles of a
   // sequence have as many places as the longest has parts, and their steps are taken as half of that at least; sums are float32 there.
-  const int64_t split = (2 * s.workgroups + c.kv_heads - 1) / c.kv_heads, chunks = s.listed ? split : 2 * split + 16;
-  s.split_tiles = s.may_split ? std::min<int64_t>(s.tiles, split) : 0;
-  s.slots = s.may_split ? s.split_tiles + chunks : 0;
+  const int64_t split = (2 * s.workgroups + c.kv_heads - 1) / c.kv_heads, chunks = listed ? split : 2 * split + 16;
+  s.split_tiles = may_split ? std::min<int64_t>(s.tiles, split) : 0;
+  s.slots = may_split ? s.split_tiles + chunks : 0;
   s.items = std::max<int64_t>(s.tiles, s.slots);
   auto up = [](uint64_t bytes) { return (bytes + 255) / 256 * 256; };
   s.bins_at = 256;
-  s.items_at = s.bins_at + up(((uint64_t)c.sequences + 1) * 4);
+  s.items_at = s.bins_at + up(((uint64_t)sequences + 1) * 4);
   s.merge_at = s.items_at + up((uint64_t)s.items * sizeof(DenseItem));
   s.stat_at = s.merge_at + up((uint64_t)s.split_tiles * sizeof(DenseMerge));
-  const uint64_t results = (uint64_t)s.slots * c.kv_heads * s.rows;
+  const uint64_t results = (uint64_t)s.slots * c.kv_heads * tile;
   s.part_at = s.stat_at + up(results * 8);
   s.workspace = s.part_at + up(results * c.head_dim * 4);
   return s;
+}
+
+}  // namespace
+
+DenseShape dense_shape(const jenga_dense_config& c) {
+  const int64_t group = c.heads / c.kv_heads, rows = c.q_rows * group;
+  // Tiles of 16 rows for a few tokens each: 16 sequences of 3 tokens over 4000 keys x 8 heads 56 us, in tiles of 128 76; 64 x 4 tokens, four heads on one of
+  // keys, 59 and 58; 64 x 20 tokens 130 and 101.  Few tokens on average may be a long prompt and many single tokens: 8000 and 300 x 1, 16 heads, 1353 and 685.
+  const int tile = c.q_rows <= 4 * (int64_t)c.sequences && rows <= 32 * (int64_t)c.sequences ? 16 : 128;
+  const int64_t workgroups = dense_shape_of(c, rows, c.sequences, tile, false, false).workgroups;
+  // full tiles that there are at least
+  const int64_t least = rows / tile;
+  return dense_shape_of(c, rows, c.sequences, tile, least * c.kv_heads < 2 * workgroups, c.sequences > 64);
+}
+
+// The most workgroups and bytes that a call with no more rows, keys and sequences has.  Neither is the larger call's own: it may have tiles enough that none is cut,
+// and fewer sequences may leave tiles of 128 rows where it has 16.
+void dense_most(const jenga_dense_config& c, int64_t* workgroups, uint64_t* workspace) {
+  const int64_t group = c.heads / c.kv_heads, rows = c.q_rows * group, few = std::min(std::min<int64_t>(rows, 4 * group * c.sequences), (int64_t)32 * c.sequences);
+  const DenseShape s[2] = {dense_shape_of(c, few, c.sequences, 16, true, false), dense_shape_of(c, rows, c.sequences, 128, true, false)};
+  *workgroups = std::max(s[0].items, s[1].items) * c.kv_heads;
+  *workspace = std::max(s[0].workspace, s[1].workspace);
 }
 
 }  // namespace jenga
@@ -642,6 +665,15 @@ int jenga_dense_attn_workspace(const jenga_dense_config* c, uint64_t* bytes) {
   if (why != JENGA_OK) return why;
   *bytes = jenga::dense_shape(*c).workspace;
   return JENGA_OK;
+}
+
+int jenga_dense_attn_workspace_up_to(const jenga_dense_config* c, uint64_t* bytes) {
+  if (!bytes) return JENGA_EINVAL;
+  const int why = jenga::dense_config_ok(c);
+  if (why != JENGA_OK) return why;
+  int64_t workgroups;
+  jenga::dense_most(*c, &workgroups, bytes);
+  return workgroups > jenga::DENSE_WORKGROUPS ? JENGA_EUNSUPPORTED : JENGA_OK;
 }
 
 int jenga_layer_norm_grad_workspace(const jenga_norm_config* c, uint64_t* bytes) {

@@ -194,7 +194,8 @@ class DenseBlock:
             self.total, self.out = [torch.empty((rows, hidden), dtype=torch.bfloat16, device=dev) for _ in range(2)]
             self.qkv = torch.empty((rows, heads + 2 * kv_heads, head_dim), dtype=torch.bfloat16, device=dev)
             self.attended = torch.empty((rows, heads, head_dim), dtype=torch.bfloat16, device=dev)
-            self.room = torch.empty(B.jenga_dense_attn_workspace(rows, rows, sequences, heads, kv_heads, head_dim), dtype=torch.uint8, device=dev)
+            self.room = torch.empty(B.jenga_dense_attn_workspace_up_to(rows, rows, sequences, heads, kv_heads, head_dim), dtype=torch.uint8,
+                                    device=dev)
 
     def _room(self, rows, cols):
         padded = B.padded_columns(cols)
