@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 @pytest.mark.parametrize("rows,sequences,lens", [(20000, 8, [60, 1, 139]), (20000, 8, [3000, 2000]), (64, 16, [64]), (64, 16, [40, 3]), (9000, 100, [1] * 70),
                                                  (9000, 100, [8999])])
-@pytest.mark.parametrize("heads,kv_heads,d", [(6, 2, 64), (5, 5, 128)])
+@pytest.mark.parametrize("heads,kv_heads,d", [(6, 2, 64), (5, 5, 128), (40, 8, 64)])
 def test_shorter_batches(rows, sequences, lens, heads, kv_heads, d):
     n, hidden = sum(lens), 192
     starts = torch.tensor([0] + torch.tensor(lens).cumsum(0).tolist(), dtype=torch.int32, device="cuda:0")
