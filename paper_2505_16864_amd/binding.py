@@ -328,6 +328,13 @@ def _whole(t, what, shape, dtype):
     _refuse(what, "shape %s, type %s" % (tuple(t.shape), t.dtype))
 
 
+def _room(workspace, what):
+    """Address and bytes of a workspace.  One with gaps or repeats has fewer bytes, or has them elsewhere, than its elements say."""
+    if not workspace.is_contiguous():
+        _refuse(what, "a workspace with gaps")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def scale_columns(cols):
     """Bytes of a row of scales of an 8-bit tensor with `cols` columns."""
     return -(-cols // 512) * 4
@@ -447,10 +454,10 @@ def jenga_layer_norm_grad(x, dy, dx, weight, mean, rstd, dweight=None, dbias=Non
                 _refuse(what, "gradients of %d groups" % groups)
             _whole(t, what, t.shape, "f32")
     stream = _on_device(what, (x, dy, dx, weight, mean, rstd, dweight, dbias, workspace), stream)
+    at_room, room = (None, 0) if workspace is None else _room(workspace, what)
     if rows:
         _check(_lib.jenga_layer_norm_grad(cfg, x.data_ptr(), dy.data_ptr(), _ptr(weight), mean.data_ptr(), rstd.data_ptr(),
-                                          dx.data_ptr(), _ptr(dweight), _ptr(dbias), _ptr(workspace),
-                                          0 if workspace is None else workspace.numel() * workspace.element_size(), stream), what)
+                                          dx.data_ptr(), _ptr(dweight), _ptr(dbias), at_room, room, stream), what)
 
 
 # The calls below are written out where the ones above share helpers: a small one costs what its Python and a launch cost.
@@ -659,7 +666,7 @@ def jenga_rms_norm_grad(total, dy, dx, weight, rstd, dtotal=None, dweight=None, 
         if dweight.get_device() != device:
             device = -1
     if workspace is not None:
-        at_room, room = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        at_room, room = _room(workspace, what)
         if workspace.get_device() != device:
             device = -1
     current = _one_gpu(what, device if device == dy.get_device() == dx.get_device() == rstd.get_device() else -1)
@@ -717,6 +724,7 @@ def jenga_dense_attn(q, k, v, out, q_start, kv_start, kv_len=None, causal=False,
             device = -1
     if workspace is None:
         _refuse(what, "a workspace is wanted")
+    at_room, room = _room(workspace, what)
     if not device == k.get_device() == v.get_device() == out.get_device() == q_start.get_device() == kv_start.get_device() == \
             workspace.get_device():
         device = -1
@@ -727,8 +735,7 @@ def jenga_dense_attn(q, k, v, out, q_start, kv_start, kv_len=None, causal=False,
         # without keys there is nothing to read, but the call wants addresses
         here = q.data_ptr()
         status = _lib.jenga_dense_attn(cfg, here, k.data_ptr() or here, v.data_ptr() or here, q_start.data_ptr(), kv_start.data_ptr(), at_len,
-                                       out.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                                       current if stream is None else stream)
+                                       out.data_ptr(), at_room, room, current if stream is None else stream)
         if status:
             raise JengaError(status, what)
 
