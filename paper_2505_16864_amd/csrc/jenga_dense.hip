@@ -54,6 +54,7 @@ template <>
 struct Type<__bf16> {
   typedef bf16x8 eight;
   static constexpr float SUM_MAX = 1073741824.0f;   // 2^30
+  static constexpr bool WIDE = true;                // values may be as large as float32 holds
   static constexpr uint32_t EXPONENT = 0x7F807F80u;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const f32x2 v = {lo, hi};
@@ -76,6 +77,7 @@ template <>
 struct Type<_Float16> {
   typedef f16x8 eight;
   static constexpr float SUM_MAX = 32768.0f;   // below the largest fp16
+  static constexpr bool WIDE = false;
   static constexpr uint32_t EXPONENT = 0x7C007C00u;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const f32x2 v = {lo, hi};
@@ -428,20 +430,38 @@ __device__ __forceinline__ u32x4 keys_of_step(const uint16_t* base, int64_t row_
 // registers, three workgroups a compute unit.
 //
 // SUM_MAX: a step forms its probabilities against the reference as it stands and only looks at their sum.  While a lane's 32 add up to at
-// most SUM_MAX, they, their float32 sums and the float32 products made of them can all be represented.  A sum above it, infinite or
+// most SUM_MAX, they and their float32 sums can be represented.  A sum above it, infinite or
 // undefined sends the step down the exact path: logits again, the row's maximum, what has been added up rescaled, probabilities <= 1.  The first
 // step of a row starts there, so the reference never exceeds the largest logit seen and the largest term is never lost to underflow.
+//
+// Sums of such probabilities times values can be represented, too, if the values are fp16, or bf16 below 2^70.  Where a tile of bf16 ends with one
+// that is not finite it is made again, lifted: with references 2^32 above the maximum, probabilities <= 2^-32, a lane's sum of a step <= 2^-27 and the sum over
+// 2^31 keys <= 1, so that what is added up stays below the largest value.  (Results below 2^-83 lose bits there, and tiles that see an infinity or a NaN take
+// twice their time.)  The look at the sums costs 0.6 % of the nine prompts, 2.5 % of 512 keys, a microsecond of 40 of single tokens.
+constexpr float LIFT = 32.0f, LIFTED_MAX = 7.450580596923828125e-09f;   // 2^-27
+template <int N, typename V>
+__device__ __forceinline__ bool any_not_finite(const V (&v)[N]) {   // times 0 these are NaN, others 0
+  float sum[4] = {};
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(V) / 4); ++e) sum[e & 3] = fmaf(v[i][e], 0.f, sum[e & 3]);
+  return !((sum[0] + sum[1]) + (sum[2] + sum[3]) == 0.f);
+}
+
 template <typename T, int D, bool ALIGNED>
 __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(DenseArgs a) {
   typedef typename Type<T>::eight eight;
   constexpr int KEYS = 64, KS = D / 16, DT = D / 32, MH = KEYS / 32, PH = KEYS / 16, CH = D / 8;
   constexpr int CHUNKS = KEYS * CH, COPIES = CHUNKS / 256, ROWS_PER_COPY = 256 / CH;
   __shared__ __attribute__((aligned(256))) u32x4 Ks[2 * CHUNKS];
+  __shared__ int again;
   u32x4* Vs = Ks + CHUNKS;
   const int index = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - index * a.kv_heads;
   DenseItem it;
   if (!find_item(a, index, &it)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hl = lane >> 5, ql = lane & 31;
+  if (tid == 0) again = 0;
   int row = it.row0 + 32 * wave + ql;
   Row r = row_at(a, it, kv_head, row);
   // keys that all rows of the tile see
@@ -484,17 +504,25 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(Dens
   };
   auto landed = []() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); };
 
-  float m_run = r.limit > it.begin ? -__builtin_inff() : 0.f, l_run = 0.f;   // 0: a row that sees none of these keys
-  bool unset = true, taken = false;
+  float m_run, l_run;
+  bool unset, taken = false, lifted = false;
   f32x16 O[DT];
+  auto restart = [&]() {
+    uint32_t from = k_from;
+    asm volatile("" : "+v"(from));   // addresses of its own: kept for both places they cost 8 registers more than there are
+    if (it.begin < it.end) copy(k0, a.k_row, from, Ks, ks_wave, it.begin);
+    m_run = r.limit > it.begin ? -__builtin_inff() : 0.f;   // 0: a row that sees none of these keys
+    l_run = 0.f;
+    unset = true;
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) O[dt] = 0.f;
+    for (int dt = 0; dt < DT; ++dt) O[dt] = 0.f;
+  };
 
   const uint32_t ks_lane = lds_address(Ks) + ql * (2 * D) + (hl ^ k_swizzle(ql)) * 16;
   const int v_row = 4 * hl + ((lane >> 2) & 3);
   const uint32_t vs_lane = lds_address(Vs) + v_row * (2 * D) + v_swizzle(v_row) * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
 
-  if (it.begin < it.end) copy(k0, a.k_row, k_from, Ks, ks_wave, it.begin);
+  restart();
   for (int key = it.begin; key < it.end; key += KEYS) {
     landed();
     __syncthreads();   // K of this step is in LDS; every wavefront is past the products of the step before
@@ -541,7 +569,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(Dens
     if (!unset) {
       logits();
       sum = probabilities(-m_run);
-      in_range = __ballot(!(sum <= Type<T>::SUM_MAX)) == 0;
+      in_range = __ballot(!(sum <= (lifted ? LIFTED_MAX : Type<T>::SUM_MAX))) == 0;
     }
     if (!in_range) {
       logits();
@@ -551,7 +579,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(Dens
 #pragma unroll
         for (int e = 0; e < 16; ++e) top = fmaxf(top, S[m][e]);
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float m_new = fmaxf(m_run, top * a.scale_log2e);
+      const float m_new = fmaxf(m_run, fmaf(top, a.scale_log2e, lifted ? LIFT : 0.f));
       const float alpha = m_new == m_run ? 1.0f : exp2_of(m_run - m_new);
       l_run *= alpha;
       m_run = m_new;
@@ -577,6 +605,15 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(Dens
     for (int p = 0; p < PH; ++p)
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul32(__builtin_bit_cast(eight, v_fragment(dt, p)), pb[p], O[dt]);
+    if (Type<T>::WIDE && key + KEYS >= it.end && !lifted) {   // after the last step
+      if (any_not_finite(O)) again = 1;
+      __syncthreads();   // every wavefront has read K and V
+      lifted = __builtin_amdgcn_readfirstlane(again);
+      if (lifted) {
+        restart();
+        key = it.begin - KEYS;
+      }
+    }
   }
   if (a.take_out && __syncthreads_or(taken)) {   // what was taken out, to the rows that see it: it makes of a sum what it is itself
     for (int key = it.begin + max(all_see - it.begin, 0) / KEYS * KEYS; key < min(it.end, r.limit); ++key) {
@@ -603,7 +640,7 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void dense_tiles_kernel(Dens
   // Through LDS, so that a store takes whole rows: stored from here, 16 bytes of 32 rows at a time and through the caches, 62400
   // rows x 12 heads took 98 us for a single key instead of 75, which is what reading q and writing out takes.
   const float inv = l_all > 0.f ? 1.0f / l_all : l_all == 0.f ? 0.f : l_all;   // NaN stays
-  __syncthreads();   // every wavefront has read K and V
+  if (!Type<T>::WIDE || lifted) __syncthreads();   // as above
   const uint32_t room = lds_address(Ks) + wave * (64 * D);   // 32 rows
   auto turned = [](int row) { return D == 128 ? row & 15 : row & 7; };
 #pragma unroll
@@ -681,90 +718,98 @@ __global__ __launch_bounds__(64 * ROWS_WAVES) void dense_rows_kernel(DenseArgs a
     copy(k0, a.k_row, k_swizzle, key, lds + stage * 2 * BYTES);
     copy(v0, a.v_row, v_swizzle, key, lds + stage * 2 * BYTES + BYTES);
   };
-  float m_run = r.limit > it.begin ? -__builtin_inff() : 0.f, l_run = 0.f;
-  bool unset = true, taken = false;
+  float m_run, l_run;
+  bool unset, taken = false, lifted = false;
   f32x4 O[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt) O[dt] = 0.f;
   const uint32_t k_lane = i16 * (2 * D) + (g ^ k_swizzle(i16)) * 16;
   const int v_row = 4 * g + ((lane >> 2) & 3);
   const uint32_t v_lane = BYTES + v_row * (2 * D) + (((lane >> 1) & 1) ^ v_swizzle(v_row)) * 16 + (lane & 1) * 8;
 
   const int first_key = it.begin + KEYS * wave;
-  int key = first_key, stage = 0;
-  if (key < it.end) {
-    copy_step(key, 0);
-    copy_step(key + WAVES * KEYS, 1);
-  }
-  for (; key < it.end; key += WAVES * KEYS, stage ^= 1) {
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(ALIGNED ? 2 * COPIES : 0) : "memory");
-    const uint32_t at = lds + stage * 2 * BYTES;
-    const bool masked = key + KEYS > all_see;
-    if (masked && a.take_out) {
+  // two turns that only copy, in front
+  for (int key = first_key - 2 * WAVES * KEYS, stage = 0; key < it.end; key += WAVES * KEYS, stage ^= 1) {
+    if (key < first_key) {
+      m_run = r.limit > it.begin ? -__builtin_inff() : 0.f;
+      l_run = 0.f;
+      unset = true;
 #pragma unroll
-      for (int c = 0; c < COPIES; ++c) taken |= take_out<T>(at + BYTES + c * 1024 + lane * 16);
-    }
-    f32x4 S[2] = {};
+      for (int dt = 0; dt < DT; ++dt) O[dt] = 0.f;
+    } else {
+      asm volatile("s_waitcnt vmcnt(%0)" : : "n"(ALIGNED ? 2 * COPIES : 0) : "memory");
+      const uint32_t at = lds + stage * 2 * BYTES;
+      const bool masked = key + KEYS > all_see;
+      if (masked && a.take_out) {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-        S[m] = Type<T>::mul16(__builtin_bit_cast(eight, piece16(at + (k_lane ^ (ks * 64)) + m * 32 * D)), qf[ks], S[m]);
-    if (masked) {
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (key + 16 * m + 4 * g + e >= r.limit) S[m][e] = -__builtin_inff();
-    }
-    eight pb;
-    auto probabilities = [&](float off) {
-      float s = 0.f;
-      u32x4 w;
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          p[e] = exp2_of(fmaf(S[m][e], a.scale_log2e, off));
-          s += p[e];
-        }
-        w[2 * m] = Type<T>::pack(p[0], p[1]);
-        w[2 * m + 1] = Type<T>::pack(p[2], p[3]);
+        for (int c = 0; c < COPIES; ++c) taken |= take_out<T>(at + BYTES + c * 1024 + lane * 16);
       }
-      pb = __builtin_bit_cast(eight, w);
-      return s;
-    };
-    float sum = 0.f;
-    bool in_range = false;
-    if (!unset) {
-      sum = probabilities(-m_run);
-      in_range = __ballot(!(sum <= Type<T>::SUM_MAX)) == 0;
-    }
-    if (!in_range) {
-      float top = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float m_new = fmaxf(m_run, top * a.scale_log2e);
-      const float alpha = m_new == m_run ? 1.0f : exp2_of(m_run - m_new);
-      l_run *= alpha;
-      m_run = m_new;
-      unset = __ballot(m_run == -__builtin_inff()) != 0;
+      f32x4 S[2] = {};
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) O[dt] *= alpha;
-      sum = probabilities(m_run == -__builtin_inff() ? 0.f : -m_run);
-    }
-    l_run += sum;
-    // channels 16 dt to + 15: pieces 2 dt and 2 dt + 1 of the row, before their rotation
-    auto v_fragment = [&](int dt) {
-      const uint32_t from = at + (v_lane ^ (dt * 32));
-      const u32x2 lo = columns(from), hi = columns(from + 32 * D);
-      return (u32x4){lo[0], lo[1], hi[0], hi[1]};
-    };
+      for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul16(__builtin_bit_cast(eight, v_fragment(dt)), pb, O[dt]);
-    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // this stage has been read
-    copy_step(key + 2 * WAVES * KEYS, stage);
+        for (int m = 0; m < 2; ++m)
+          S[m] = Type<T>::mul16(__builtin_bit_cast(eight, piece16(at + (k_lane ^ (ks * 64)) + m * 32 * D)), qf[ks], S[m]);
+      if (masked) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (key + 16 * m + 4 * g + e >= r.limit) S[m][e] = -__builtin_inff();
+      }
+      eight pb;
+      auto probabilities = [&](float off) {
+        float s = 0.f;
+        u32x4 w;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[e] = exp2_of(fmaf(S[m][e], a.scale_log2e, off));
+            s += p[e];
+          }
+          w[2 * m] = Type<T>::pack(p[0], p[1]);
+          w[2 * m + 1] = Type<T>::pack(p[2], p[3]);
+        }
+        pb = __builtin_bit_cast(eight, w);
+        return s;
+      };
+      float sum = 0.f;
+      bool in_range = false;
+      if (!unset) {
+        sum = probabilities(-m_run);
+        in_range = __ballot(!(sum <= (lifted ? LIFTED_MAX : Type<T>::SUM_MAX))) == 0;
+      }
+      if (!in_range) {
+        float top = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])), fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m_new = fmaxf(m_run, fmaf(top, a.scale_log2e, lifted ? LIFT : 0.f));
+        const float alpha = m_new == m_run ? 1.0f : exp2_of(m_run - m_new);
+        l_run *= alpha;
+        m_run = m_new;
+        unset = __ballot(m_run == -__builtin_inff()) != 0;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) O[dt] *= alpha;
+        sum = probabilities(m_run == -__builtin_inff() ? 0.f : -m_run);
+      }
+      l_run += sum;
+      // channels 16 dt to + 15: pieces 2 dt and 2 dt + 1 of the row, before their rotation
+      auto v_fragment = [&](int dt) {
+        const uint32_t from = at + (v_lane ^ (dt * 32));
+        const u32x2 lo = columns(from), hi = columns(from + 32 * D);
+        return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+      };
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) O[dt] = Type<T>::mul16(__builtin_bit_cast(eight, v_fragment(dt)), pb, O[dt]);
+      asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // this stage has been read
+      if (Type<T>::WIDE && key + WAVES * KEYS >= it.end && !lifted && __ballot(any_not_finite(O)) != 0) {   // after the last step
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+        lifted = true;
+        key = first_key - 3 * WAVES * KEYS;
+        continue;
+      }
+    }
+    if (first_key < it.end) copy_step(key + 2 * WAVES * KEYS, stage);
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");   // nothing is on its way into LDS
 
@@ -801,7 +846,7 @@ __global__ __launch_bounds__(64 * ROWS_WAVES) void dense_rows_kernel(DenseArgs a
   for (int w = 0; w < WAVES; ++w) {
     const float l = stats[w][row][1];
     if (l == 0.f) continue;
-    const float by = exp2_of(stats[w][row][0] - m_all);
+    const float by = exp2_of(stats[w][row][0] - m_all) * (1.0f / WAVES);   // so that the sum of finite results is finite
     l_all = fmaf(l, by, l_all);
     const float* from = (const float*)(tiles + w * ROOM) + row * D + c0;
 #pragma unroll
@@ -847,7 +892,7 @@ __global__ __launch_bounds__(256) void dense_merge_rows_kernel(DenseArgs a) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) top_here = fmaxf(top_here, __shfl_xor(top_here, d));
     const float top_new = fmaxf(top, top_here), alpha = top_new == top ? 1.0f : exp2_of(top - top_new);
-    const float weight = sum != 0.f ? exp2_of(m - top_new) : 0.f;
+    const float weight = sum != 0.f ? exp2_of(m - top_new) * (1.0f / MOST_PARTS) : 0.f;   // so that the sum of finite results is finite
     top = top_new;
     l = l * alpha + wave_sum_f32(sum * weight);
     o *= alpha;
@@ -909,7 +954,7 @@ __global__ __launch_bounds__(256) void dense_merge_tiles_kernel(DenseArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float weight = s[i][1] != 0.f && p + i < it.parts ? exp2_of(s[i][0] - top) : 0.f;
+      const float weight = s[i][1] != 0.f && p + i < it.parts ? exp2_of(s[i][0] - top) * (1.0f / MOST_PARTS) : 0.f;
       if (weight != 0.f) {
         l = fmaf(s[i][1], weight, l);
         o += x[i] * weight;
