@@ -558,7 +558,8 @@ typedef struct {
  * Starts and lengths are cut to what is there on the device, so that no malformed number causes an access out of range.  What rows do not
  * see does not touch them, whatever it holds.  Products of 16 bits, sums and softmax float32; the probabilities are rounded to
  * 16 bits, the sum that divides them is not.  Results do not depend on the order of execution: the same call gives the same bits.
- * JENGA_EUNSUPPORTED: another head_dim, more than 2^16 sequences, 2^12 heads or 2^30 rows with their heads, row strides above 2^23.
+ * JENGA_EUNSUPPORTED: another head_dim, more than 2^16 sequences or 2^12 heads, 2^31 rows with the heads that share keys, row strides above 2^23, or more than
+ * 2^23 workgroups: rows with all their heads / 128 (/ 16 where sequences have few rows, 4 and 32 with the heads that share keys on average) + sequences x kv_heads.
  */
 int jenga_dense_attn(const jenga_dense_config* cfg, const void* q, const void* k, const void* v, const int32_t* q_start,
                      const int32_t* kv_start, const int32_t* kv_len_or_null, void* out, void* workspace, size_t workspace_bytes,

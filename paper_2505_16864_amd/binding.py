@@ -559,7 +559,7 @@ def _rms_weight(weight, what, cols):
 
 def jenga_rms_norm(x, y, weight=None, residual=None, total=None, y_scale=None, rstd=None, weight_offset=0.0, eps=1e-6, stream=None):
     """x, residual, total [rows, cols] or [rows, heads, cols] of one type, each with strides of its own; y the same, or of [rows, cols] an
-    8-bit (e4m3) or 4-bit (uint8) tensor with its scales in y_scale; weight [cols]; rstd float32 [rows] or [rows, heads].  total, or y,
+    8-bit (e4m3; its bytes will not do here) or 4-bit (uint8) tensor with its scales in y_scale; weight [cols]; rstd float32 [rows] or [rows, heads].  total, or y,
     may be x or residual."""
     what = "jenga_rms_norm"
     dtype, device = x.dtype, x.get_device()

@@ -44,3 +44,17 @@ def test_refusals():
     with pytest.raises(J.JengaError) as e:
         J.jenga_dense_attn_workspace_up_to(16, 16, 1, 4, 3, 64)
     assert e.value.status == -1
+
+
+# The limits that the header names: rows with the heads that share keys, and workgroups.
+@pytest.mark.parametrize("rows,sequences,heads,kv_heads,taken", [
+    ((1 << 30) // 64, 1, 64, 64, False), ((1 << 30) // 64 - 128, 1, 64, 64, True), ((1 << 31) // 8 - 1, 1, 8, 1, False), ((1 << 30) // 8 - 128 * 8, 1, 8, 1, True),
+    (1 << 20, 1 << 16, 128, 128, False), (1 << 20, (1 << 16) - (1 << 13), 128, 128, True), (1 << 16, 1 << 16, 40, 40, True), (1 << 16, 1 << 16, 121, 121, False),
+    (1 << 16, 1 << 16, 120, 120, True)])
+def test_limits(rows, sequences, heads, kv_heads, taken):
+    if taken:
+        assert J.jenga_dense_attn_workspace(rows, rows, sequences, heads, kv_heads, 64) > 0
+        return
+    with pytest.raises(J.JengaError) as e:
+        J.jenga_dense_attn_workspace(rows, rows, sequences, heads, kv_heads, 64)
+    assert e.value.status == -2
