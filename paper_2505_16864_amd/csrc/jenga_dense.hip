@@ -667,7 +667,7 @@ constexpr int ROWS_WAVES = 2;
 
 // Few rows: the keys are read once and are what takes the time.  Each wavefront takes 32 keys of every 32 x WAVES with LDS of its own,
 // two steps deep, so that nothing but its own copies makes it wait; they join at the end.  Two wavefronts a workgroup, 64 KB of LDS at D = 128: 16
-// sequences of 1 to 8192 keys x 8 heads 40.6 us and 6.6 to join, 4.7 TB/s; 64 x 2000 5.2 TB/s.  (Four a workgroup, one workgroup on a compute unit: 45.2.)
+// sequences of 1 to 8192 keys x 8 heads 41.8 us and 6.6 to join, 4.6 TB/s; 64 x 2000 x 8, whole calls, 4.8 TB/s.  (Four a workgroup, one workgroup on a compute unit: 45.2.)
 template <typename T, int D, bool ALIGNED>
 __global__ __launch_bounds__(64 * ROWS_WAVES) void dense_rows_kernel(DenseArgs a) {
   typedef typename Type<T>::eight eight;

@@ -153,7 +153,7 @@ __device__ __forceinline__ void copy_pieces(bool wanted, const u32x4& buffer, ui
 // the barrier is: behind it the next tile is complete, and the one STAGES blocks on goes over this one.
 //
 // 33272 x 15360 x 5120 to bf16: 1.40 to 1.48 ms, 3.5 to 3.7 PFLOP/s (all-zero operands 1.15); without copies of operands 1.13, without scales
-// 1.24, without stores 1.45 where it took 1.65: the way into LDS, and behind it the package power.  Products of one half before those of the other
+// 1.24, without stores 1.45 where it took 1.65: no part bounds it alone.  A wavefront a SIMD does them one after the other.  Products of one half before those of the other
 // (two accumulations into a tile apart) and starts spread over a tile's time changed nothing; scales shifted at their first use 1.54.
 //
 // A copy instruction takes 8 whole rows of 128 bytes: first their left halves, then the right ones.  Where k has an odd number of halves,

@@ -468,6 +468,10 @@ void run_rows(const RmsArgs& a, hipStream_t st) {
   rms_kernel<X, P, OUT, LANES, NV><<<(unsigned)std::min<int64_t>((a.rows + AT_ONCE - 1) / AT_ONCE, most), THREADS, 0, st>>>(a);
 }
 
+// One piece a thread up to 2048 columns, but three pieces of a wavefront for 1025 to 1536 (63424 x 1536 bf16 150 us, one piece of three wavefronts 178); beyond, shapes of
+// whole wavefronts without many idle lanes.  120 M values bf16 with residual and sum, us, to the same type / 8 bits / 4 bits, with the shape taken and with another:
+// 1536 columns 64 x 3 182 / 153 / 145, 192 x 1 194 / 193 / 181; 4096 256 x 2 181 / 153 / 141, 512 x 1 185 / 160 / 147; 5120 768 x 1 185 / 162 / 156, 640 x 1
+// 188 / 162 / 153; 8192 512 x 2 176 / 155 / 146, 1024 x 1 178 / 169 / 165; 12288 512 x 3 184 / 158 / 149, 768 x 2 178 / 196 / 192.
 template <typename X, typename P, Out OUT>
 int run_rms(const RmsArgs& a, hipStream_t st) {
   if (a.cols > MOST_COLS)
@@ -498,8 +502,9 @@ int run_grad_rows(const RmsArgs& a, hipStream_t st) {
 }
 
 // One piece a thread where rows have exact shapes for it: gradient of 63424 x 1536 bf16 in three pieces of a wavefront 225 us, in one of
-// three 158; 33272 x 5120 510 -> 266, 12000 x 8192 234 -> 146.  (The forward pass does not mind: 150 and 178 at 1536.)  The last two shapes keep 10 to 21
-// registers in scratch, and still beat the kernel that reads rows again: 6000 x 10000 float32 304 and 337, 6000 x 16000 bf16 228 and 348
+// three 158; 33272 x 5120 510 -> 266, 12000 x 8192 234 -> 146.  2049 to 3584 columns take two pieces of four wavefronts, which differ little from one of
+// eight (120 M values bf16, 2560 columns 165 and 159 us, 3584 141 and 136, 4096, which takes the latter, 146 and 136; 60 M float32 140 and 138, 140 and 140).  The last
+// two shapes keep 10 to 21 registers in scratch, and still beat the kernel that reads rows again: 6000 x 10000 float32 304 and 337, 6000 x 16000 bf16 228 and 348
 // (4000 x 16000 float32, with 68, does not: 414 and 335).
 template <typename X, typename P>
 int run_grad(const RmsArgs& a, float* dweight, hipStream_t st) {
