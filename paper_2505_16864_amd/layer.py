@@ -210,7 +210,7 @@ class DenseBlock:
     def forward(self, x, starts, residual=None, cells=None):
         """x, residual bf16 [n, hidden], starts int32 [sequences + 1] on the device: rows of each sequence; cells int32 [n, 3] where there are
         rotary positions.  Returns the sum of x and residual and what the block adds to it, bf16 [n, hidden], overwritten by the next
-        call.  All on torch's current stream."""
+        call; for rows in front of the first sequence and behind the last what is added has no meaning.  All on torch's current stream."""
         n = x.shape[0]
         if n > self.rows or starts.numel() - 1 > self.sequences:
             raise ValueError("%d rows of %d sequences for a block of %d and %d" % (n, starts.numel() - 1, self.rows, self.sequences))
